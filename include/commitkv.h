@@ -19,6 +19,16 @@
  *                             Sec. 3.1, Eq. (4): the same indices applied to
  *                             keys, values and absolute positions.
  *
+ * and the calls with which a serving step reads such caches (Sec. 4.1: a
+ * batch of sequences over a paged pool):
+ *
+ *   ckv_build_slots           block tables and slot tables of a batch, built
+ *                             on the device from its lengths.
+ *   ckv_attend_window         attention of a ragged batch, with a sliding
+ *                             window and first tokens that stay visible.
+ *   ckv_attend_shared         attention of a batch whose sequences begin with
+ *                             the same tokens, read once for all.
+ *
  * Conventions shared by every call
  * --------------------------------
  *  - Tensor pointers are DEVICE pointers unless a field says "host".  The
@@ -513,6 +523,180 @@ int ckv_select_and_compact(ckv_ctx* ctx, const ckv_cache_view* in,
                            const ckv_budget* budget, const ckv_cache_view* out,
                            int32_t* kept_idx, int32_t* n_kept,
                            uint8_t* token_state);
+
+/* ------------------------------------------------- serving over the caches */
+
+/* Element types of a batch's keys, values, queries and outputs. */
+#define CKV_BF16 0
+#define CKV_F16 1
+
+/* Resident caches of ONE layer of n_seq sequences.  Key (s, g, t, e) is
+ * k[s*seq_stride + g*head_stride + t*tok_stride + e] for sequence s, KV head
+ * g, token t < n_tokens[s]; same for v.  With `slot` the storage is a paged
+ * pool that all sequences share: the key is k[g*head_stride + row*tok_stride
+ * + e] with row = slot[s*slot_stride + t], a row of the pool's pool_rows rows
+ * (values outside are clamped to the last row: wrong but in bounds).
+ * n_tokens is on the DEVICE, so that a captured step serves growing caches;
+ * max_tokens is the host's bound (larger and negative counts are clamped to
+ * [0, max_tokens]; slot and pos rows hold max_tokens entries at least).
+ * pos[s*pos_stride + t] is the token's absolute position, >= 0 and ascending
+ * in t (with another order the calls stay in bounds, and which tokens a row
+ * sees is undefined).  NULL: token t is at position t, or, in
+ * ckv_attend_shared, at position t behind the shared tokens. */
+typedef struct ckv_batch_view {
+  const uint16_t* k;
+  const uint16_t* v;
+  int64_t seq_stride;        /* elements; ignored with slot */
+  int64_t head_stride;       /* elements */
+  int64_t tok_stride;        /* elements */
+  const int32_t* slot;       /* device int32, or NULL: contiguous */
+  int64_t slot_stride;       /* entries between the rows of two sequences */
+  const int32_t* pos;        /* device int32, or NULL */
+  int64_t pos_stride;
+  const int32_t* n_tokens;   /* device int32[n_seq] */
+  int32_t n_seq;
+  int32_t max_tokens;
+  int32_t pool_rows;         /* with slot */
+  int32_t n_kv_heads;
+  int32_t head_dim;          /* d: 64 or 128 */
+  int32_t dtype;             /* CKV_BF16 or CKV_F16 */
+} ckv_batch_view;
+
+/* Query rows of a batch, packed: query (r, h, e) is q[r*row_stride +
+ * h*head_stride + e] for row r < n_rows; sequence s owns rows cu_rows[s] to
+ * cu_rows[s+1]-1 (device int32[n_seq+1], ascending, clamped into [0, n_rows];
+ * a sequence may own none).  qpos[r] is the row's absolute position; NULL:
+ * the rows of a sequence are its last tokens, one each (row j of R is token
+ * n_tokens - R + j; a row before token 0 of a cache with positions sees
+ * nothing).  Query head h reads KV head h / (n_q_heads / n_kv_heads).
+ * max_rows is the host's estimate of the most rows a sequence owns; it picks
+ * the kernels (1: single tokens), and any count is served right. */
+typedef struct ckv_query_view {
+  const uint16_t* q;
+  int64_t row_stride;        /* elements */
+  int64_t head_stride;       /* elements */
+  const int32_t* cu_rows;    /* device int32[n_seq + 1] */
+  const int32_t* qpos;       /* device int32[n_rows], or NULL */
+  int32_t n_q_heads;         /* a multiple of n_kv_heads */
+  int32_t n_rows;
+  int32_t max_rows;          /* >= 1 */
+  float scale;               /* softmax scale; <= 0 selects 1/sqrt(head_dim) */
+} ckv_query_view;
+
+/*
+ * Attention of a ragged batch over its caches: prompts, chunks and single
+ * tokens, in any mixture.  Row r at position p sees token t at position p_t iff
+ *   p_t <= p  and  (window == 0  or  p - p_t < window  or  p_t < n_sink):
+ * the last `window` positions, the row's own among them, and the first n_sink
+ * positions of the sequence, which stay visible; window 0 hides nothing.
+ *   lse = log sum_t exp(scale * q.k_t),  o = sum_t exp(scale * q.k_t - lse) v_t
+ * over the tokens seen.  A row that sees none (or whose every logit is -inf)
+ * gets o = 0 and lse = -inf.
+ *
+ * Outputs (device): o [n_rows * n_q_heads * head_dim], of the batch's type,
+ * 16-byte aligned; lse float32 [n_rows * n_q_heads], optional (NULL).  Rows of
+ * no sequence are left as they were.
+ * Values, keys and slots of tokens that no row of a sequence sees do not
+ * reach its outputs, whatever they hold.
+ * Precision: float32 logits, maxima, sums and accumulation; softmax weights
+ * rounded to the batch's type before they multiply the values.
+ *
+ * The call reads counts and lengths on the device only, so a captured step
+ * replays with grown caches.  Partial sums live in a workspace of the context
+ * that later calls share: calls and replays of one context that overlap in
+ * time need contexts of their own.  Memory a captured graph refers to is kept
+ * until ckv_destroy, and an equal call made before the capture (the same
+ * n_seq, n_rows, max_rows, heads) leaves the workspace it needs.
+ * Under a workspace limit that leaves no room for partial sums the call runs
+ * without splitting sequences (more slowly, the same results up to rounding).
+ *
+ * Errors: CKV_ERR_ARG for NULL pointers, misaligned rows, an unknown type, a
+ * negative window or n_sink, outputs that overlap the queries; CKV_ERR_SHAPE
+ * for head counts, widths and strides.
+ */
+int ckv_attend_window(ckv_ctx* ctx, const ckv_batch_view* kv,
+                      const ckv_query_view* q, int32_t window, int32_t n_sink,
+                      void* o, float* lse);
+
+/*
+ * The same for a batch whose sequences share their first tokens (a system
+ * prompt, the samples of one prompt): `prefix` is a view of ONE sequence (n_seq
+ * 1) that holds the shared tokens once, `kv` the tokens of each sequence
+ * behind them (none at all is allowed).  Every row attends to the prefix and
+ * to its own sequence's tokens as to one cache: what it sees is p_t <= p
+ * over both.  Prefix and kv agree in type, heads and head_dim, and may lie in
+ * one pool.  Prefix keys and values are read once for the rows of all
+ * sequences; the two parts are joined by their maxima and sums in float32.
+ * Outputs, precision, workspace, capture and errors as for
+ * ckv_attend_window.
+ */
+int ckv_attend_shared(ckv_ctx* ctx, const ckv_batch_view* prefix,
+                      const ckv_batch_view* kv, const ckv_query_view* q,
+                      void* o, float* lse);
+
+/* One step of a batch's tables over a pool of n_blocks blocks of block_size
+ * rows.  Every pointer is a device pointer. */
+typedef struct ckv_slot_step {
+  int32_t n_seq;
+  int32_t block_size;          /* rows per block, >= 1 */
+  int32_t n_blocks;            /* blocks of the pool; n_blocks * block_size < 2^31 */
+  int32_t max_new;             /* entries of new_row and new_pos */
+  /* inputs */
+  const int32_t* n_tokens;     /* int32[n_seq]: resident tokens */
+  const int32_t* n_new;        /* int32[n_seq]: tokens that join; -1: the sequence ends */
+  const int32_t* next_pos;     /* int32[n_seq], or NULL: n_tokens; position of the first new token */
+  const int32_t* n_free;       /* int32[1]: free blocks */
+  /* updated in place */
+  int32_t* free_blocks;        /* int32[n_blocks]: stack of free blocks, top last */
+  int32_t* block_table;        /* int32 [n_seq][block_stride], or NULL with block_size 1 */
+  int64_t block_stride;
+  int32_t* slot;               /* int32 [n_seq][slot_stride]: pool row of each token */
+  int32_t* pos;                /* int32 [n_seq][slot_stride], or NULL */
+  int64_t slot_stride;
+  /* outputs; none may overlap an input */
+  int32_t* n_tokens_out;       /* int32[n_seq] */
+  int32_t* n_free_out;         /* int32[1] */
+  int32_t* cu_new;             /* int32[n_seq + 1]: first new token of each sequence */
+  int32_t* new_row;            /* int32[max_new]: pool row of each new token, sequence by sequence */
+  int32_t* new_pos;            /* int32[max_new], or NULL: its position */
+  int32_t* status;             /* int32[1] */
+} ckv_slot_step;
+
+/* ckv_slot_step.status */
+#define CKV_SLOTS_OK 0
+#define CKV_SLOTS_NO_BLOCKS 1  /* the step needs more blocks than are free */
+#define CKV_SLOTS_TABLE 2      /* a sequence would pass slot_stride or block_stride * block_size */
+#define CKV_SLOTS_MAX_NEW 3    /* more than max_new new tokens */
+#define CKV_SLOTS_BAD_COUNT 4  /* a negative n_tokens, an n_new below -1, n_free outside [0, n_blocks] */
+
+/*
+ * Places the new tokens of a batch in the pool and writes the tables that the
+ * other calls read, from lengths on the device.  Sequence s holds
+ * ceil(n_tokens / block_size) blocks, block_table[s][0..]; token t lives in
+ * row block_table[s][t / block_size] * block_size + t % block_size.
+ *   1. The blocks of every sequence that ends (n_new -1) go on top of the
+ *      free stack, in the order of sequences and of their blocks.
+ *   2. The blocks that the others need for n_tokens + n_new tokens come off
+ *      its top, in the same order.
+ *   3. For new token j of sequence s: slot[s][n_tokens + j] and
+ *      new_row[cu_new[s] + j] are its row, pos[s][n_tokens + j] and
+ *      new_pos[cu_new[s] + j] its position next_pos + j.
+ *   4. n_tokens_out is n_tokens + n_new, 0 for a sequence that ends.
+ * Entries of tables and lists that no step names are left as they were.
+ * cu_new with new_pos serves ckv_query_view (cu_rows, qpos), slot, pos and
+ * n_tokens_out serve ckv_batch_view.  A cache that drops single tokens
+ * (ckv_select_and_compact) has block_size 1; its slot table then is the block
+ * table (block_table NULL), re-indexed by the kept tokens.
+ * A step that cannot be done (status not 0) changes nothing: tables and stack
+ * stay, n_tokens_out and n_free_out repeat the inputs, cu_new is 0.  If
+ * several reasons hold, status names the one of highest number.  The result
+ * does not depend on scheduling.  Block numbers outside the pool are clamped
+ * into it wherever a row is formed.
+ * Errors: CKV_ERR_ARG (NULL pointers, block_size or sizes out of range,
+ * block_table missing where block_size > 1, outputs that overlap inputs or
+ * each other).
+ */
+int ckv_build_slots(ckv_ctx* ctx, const ckv_slot_step* step);
 
 #ifdef __cplusplus
 }

@@ -90,7 +90,34 @@ class AcceptedPages(ctypes.Structure):
                 ("accepted", ctypes.c_void_p), ("max_cand", ctypes.c_int32)]
 
 
+class BatchView(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("seq_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64), ("tok_stride", ctypes.c_int64), ("slot", ctypes.c_void_p),
+                ("slot_stride", ctypes.c_int64), ("pos", ctypes.c_void_p), ("pos_stride", ctypes.c_int64),
+                ("n_tokens", ctypes.c_void_p), ("n_seq", ctypes.c_int32), ("max_tokens", ctypes.c_int32),
+                ("pool_rows", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("dtype", ctypes.c_int32)]
+
+
+class QueryView(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("cu_rows", ctypes.c_void_p), ("qpos", ctypes.c_void_p), ("n_q_heads", ctypes.c_int32),
+                ("n_rows", ctypes.c_int32), ("max_rows", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class SlotStep(ctypes.Structure):
+    _fields_ = [("n_seq", ctypes.c_int32), ("block_size", ctypes.c_int32), ("n_blocks", ctypes.c_int32),
+                ("max_new", ctypes.c_int32), ("n_tokens", ctypes.c_void_p), ("n_new", ctypes.c_void_p),
+                ("next_pos", ctypes.c_void_p), ("n_free", ctypes.c_void_p), ("free_blocks", ctypes.c_void_p),
+                ("block_table", ctypes.c_void_p), ("block_stride", ctypes.c_int64), ("slot", ctypes.c_void_p),
+                ("pos", ctypes.c_void_p), ("slot_stride", ctypes.c_int64), ("n_tokens_out", ctypes.c_void_p),
+                ("n_free_out", ctypes.c_void_p), ("cu_new", ctypes.c_void_p), ("new_row", ctypes.c_void_p),
+                ("new_pos", ctypes.c_void_p), ("status", ctypes.c_void_p)]
+
+
 POOL_MAX, POOL_MEAN = 0, 1
+BF16, F16 = 0, 1
+SLOTS_OK, SLOTS_NO_BLOCKS, SLOTS_TABLE, SLOTS_MAX_NEW, SLOTS_BAD_COUNT = range(5)
 
 # ckv_event_kind and the due flags of include/commitkv_agent.h
 EVENT_REASONING, EVENT_TOOL_CALL, EVENT_OBSERVATION, EVENT_PROMPT, EVENT_ANSWER = range(5)
@@ -169,6 +196,13 @@ SIGNATURES = {
         ctypes.c_int64, ctypes.POINTER(PageList), ctypes.POINTER(PageList),
         ctypes.POINTER(ctypes.c_void_p), ctypes.POINTER(AcceptedPages), ctypes.POINTER(Budget),
         ctypes.POINTER(CacheView), ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]),
+    "ckv_attend_window": (ctypes.c_int, [
+        ctypes.c_void_p, ctypes.POINTER(BatchView), ctypes.POINTER(QueryView), ctypes.c_int32, ctypes.c_int32,
+        ctypes.c_void_p, ctypes.c_void_p]),
+    "ckv_attend_shared": (ctypes.c_int, [
+        ctypes.c_void_p, ctypes.POINTER(BatchView), ctypes.POINTER(BatchView), ctypes.POINTER(QueryView),
+        ctypes.c_void_p, ctypes.c_void_p]),
+    "ckv_build_slots": (ctypes.c_int, [ctypes.c_void_p, ctypes.POINTER(SlotStep)]),
     "ckv_agent_create": (ctypes.c_int, [ctypes.c_void_p, ctypes.POINTER(CacheView),
                                         ctypes.POINTER(CacheView), ctypes.POINTER(AgentConfig),
                                         ctypes.POINTER(ctypes.c_void_p)]),

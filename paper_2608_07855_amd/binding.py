@@ -15,7 +15,8 @@ import numpy as np
 import torch
 
 from . import _abi
-from ._abi import AcceptedPages, Budget, CacheView, KVView, PageList, Thresholds, WindowView
+from ._abi import (AcceptedPages, BatchView, Budget, CacheView, KVView, PageList, QueryView, SlotStep, Thresholds,
+                   WindowView)
 
 PAPER_THRESHOLDS = dict(tau_use=0.05, tau_dead=0.01, rho_use=0.75, rho_dead=0.25, tau_joint=0.01)
 
@@ -212,6 +213,140 @@ def cache_view(k, v, pos) -> CacheView:
     return view
 
 
+_DTYPES = {torch.bfloat16: _abi.BF16, torch.float16: _abi.F16}
+
+
+def _check_dev(t, name, dtype, dim=None, device=None):
+    if not t.is_cuda or t.dtype != dtype or (dim is not None and t.dim() != dim) or \
+            (t.numel() and t.dim() and t.shape[-1] > 1 and t.stride(-1) != 1):
+        raise ValueError(f"{name}: expected a cuda {dtype} tensor" + ("" if dim is None else f" of {dim} dims") +
+                         " with a contiguous last axis")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name} is on {t.device}, the others on {device}")
+
+
+def _check_flat(t, name, n, device=None):
+    _check_dev(t, name, torch.int32, None, device)
+    if not t.is_contiguous() or t.numel() < n:
+        raise ValueError(f"{name}: expected a contiguous tensor of {n} entries")
+
+
+def batch_view(k, v, n_tokens, *, slot=None, pos=None, max_tokens: int | None = None) -> BatchView:
+    """Caches of several sequences of one layer, bf16 or fp16.
+    Contiguous: k, v [n_seq, Hkv, capacity, d].  Paged (``slot`` int32 [n_seq,
+    stride]): k, v [Hkv, pool_rows, d], and token t of sequence s lives in row
+    slot[s, t].  n_tokens: int32 [n_seq] (device); pos: int32 [n_seq, stride]
+    or None (token t at position t); max_tokens: the most tokens a sequence
+    may have (default: as many as the tables or the storage hold)."""
+    nd = 4 if slot is None else 3
+    if k.dtype not in _DTYPES:
+        raise ValueError("k: expected bfloat16 or float16")
+    _check_dev(k, "k", k.dtype, nd)
+    _check_dev(v, "v", k.dtype, nd, k.device)
+    if k.shape != v.shape or k.stride() != v.stride():
+        raise ValueError("k and v must have the same shape and strides")
+    n = n_tokens.numel()
+    _check_flat(n_tokens, "n_tokens", n, k.device)
+    if slot is None:
+        if k.shape[0] != n:
+            raise ValueError(f"k holds {k.shape[0]} sequences, n_tokens {n}")
+        room = k.shape[2]
+    else:
+        _check_dev(slot, "slot", torch.int32, 2, k.device)
+        if slot.shape[0] != n:
+            raise ValueError(f"slot holds {slot.shape[0]} sequences, n_tokens {n}")
+        room = slot.shape[1]
+    if pos is not None:
+        _check_dev(pos, "pos", torch.int32, 2, k.device)
+        if pos.shape[0] != n:
+            raise ValueError(f"pos holds {pos.shape[0]} sequences, n_tokens {n}")
+        room = min(room, pos.shape[1])
+    most = room if max_tokens is None else int(max_tokens)
+    if not 0 <= most <= room:
+        raise ValueError(f"max_tokens {most} out of range (the tables hold {room})")
+    st = k.stride()
+    view = BatchView(k.data_ptr(), v.data_ptr(), st[0] if slot is None else 0, st[-3], st[-2],
+                     None if slot is None else slot.data_ptr(), 0 if slot is None else slot.stride(0),
+                     None if pos is None else pos.data_ptr(), 0 if pos is None else pos.stride(0),
+                     n_tokens.data_ptr(), n, most, 0 if slot is None else k.shape[-2], k.shape[-3], k.shape[-1],
+                     _DTYPES[k.dtype])
+    view._keep = (k, v, n_tokens, slot, pos)   # the struct holds raw pointers: keep the tensors alive
+    view._device, view._torch_dtype = k.device, k.dtype
+    return view
+
+
+def query_view(q, cu_rows, qpos=None, *, max_rows: int | None = None, scale: float = 0.0) -> QueryView:
+    """Packed query rows of a batch: q [n_rows, Hq, d] bf16 or fp16, sequence s
+    owning rows cu_rows[s]:cu_rows[s + 1] (int32 [n_seq + 1], device); qpos:
+    int32 [n_rows] or None (the rows of a sequence are its last tokens);
+    max_rows: the most rows of a sequence, an estimate (default: n_rows over
+    the sequences, rounded up)."""
+    if q.dtype not in _DTYPES:
+        raise ValueError("q: expected bfloat16 or float16")
+    _check_dev(q, "q", q.dtype, 3)
+    n = cu_rows.numel() - 1
+    _check_flat(cu_rows, "cu_rows", n + 1, q.device)
+    if n < 0:
+        raise ValueError("cu_rows holds n_seq + 1 entries")
+    if qpos is not None:
+        _check_flat(qpos, "qpos", q.shape[0], q.device)
+    most = max(1, -(-q.shape[0] // max(n, 1))) if max_rows is None else int(max_rows)
+    view = QueryView(q.data_ptr(), q.stride(0), q.stride(1), cu_rows.data_ptr(),
+                     None if qpos is None else qpos.data_ptr(), q.shape[1], q.shape[0], most, float(scale))
+    view._keep = (q, cu_rows, qpos)
+    view._n_seq, view._shape, view._device, view._torch_dtype = n, tuple(q.shape), q.device, q.dtype
+    return view
+
+
+def slot_step(n_tokens, n_new, free, n_free, slot, *, block_size: int, block_table=None, pos=None, next_pos=None,
+              n_tokens_out=None, n_free_out=None, cu_new=None, new_row=None, new_pos=None, status=None,
+              max_new: int | None = None) -> SlotStep:
+    """The tables of a step of ckv_build_slots (all int32, device).  free:
+    [n_blocks], a stack of which n_free [1] entries are free; slot, pos
+    [n_seq, stride]; block_table [n_seq, stride] (may be None with block_size
+    1).  Outputs are allocated here unless given; new_row and new_pos hold
+    max_new entries (default: as many as the tables could take)."""
+    n, dev = n_tokens.numel(), n_tokens.device
+    _check_flat(n_tokens, "n_tokens", n)
+    _check_flat(n_new, "n_new", n, dev)
+    _check_flat(free, "free", 0, dev)
+    _check_flat(n_free, "n_free", 1, dev)
+    for t, name in ((slot, "slot"), (pos, "pos"), (block_table, "block_table")):
+        if t is not None:
+            _check_dev(t, name, torch.int32, 2, dev)
+            if t.shape[0] != n:
+                raise ValueError(f"{name} holds {t.shape[0]} sequences, n_tokens {n}")
+    if pos is not None and (pos.shape != slot.shape or pos.stride() != slot.stride()):
+        raise ValueError("slot and pos must have the same shape and strides")
+    if next_pos is not None:
+        _check_flat(next_pos, "next_pos", n, dev)
+    if max_new is None:
+        max_new = new_row.numel() if new_row is not None else n * slot.shape[1]
+
+    def out(t, name, m):
+        if t is None:
+            return torch.empty(m, dtype=torch.int32, device=dev)
+        _check_flat(t, name, m, dev)
+        return t
+    n_tokens_out, n_free_out = out(n_tokens_out, "n_tokens_out", n), out(n_free_out, "n_free_out", 1)
+    cu_new, status = out(cu_new, "cu_new", n + 1), out(status, "status", 1)
+    new_row, new_pos = out(new_row, "new_row", max_new), out(new_pos, "new_pos", max_new)
+
+    def p(t):
+        return None if t is None else t.data_ptr()
+    # a table of one sequence may have any row stride: its width is what counts
+    def stride(t):
+        return 0 if t is None else (t.stride(0) if t.shape[0] > 1 else t.shape[1])
+    step = SlotStep(n, int(block_size), free.numel(), int(max_new), p(n_tokens), p(n_new), p(next_pos), p(n_free),
+                    p(free), p(block_table), stride(block_table), p(slot), p(pos), stride(slot), p(n_tokens_out),
+                    p(n_free_out), p(cu_new), p(new_row), p(new_pos), p(status))
+    step._keep = (n_tokens, n_new, next_pos, n_free, free, block_table, slot, pos)
+    step._device = dev
+    step._out = dict(n_tokens=n_tokens_out, n_free=n_free_out, cu_new=cu_new, new_row=new_row, new_pos=new_pos,
+                     status=status)
+    return step
+
+
 def _f32(n, device, fill=None):
     t = torch.empty(n, dtype=torch.float32, device=device)
     if fill is not None:
@@ -401,6 +536,64 @@ def ckv_select_and_compact(ctx: Context, k_in, v_in, pos_in, n_tokens, score, re
         ctypes.byref(cout) if cout is not None else None, _ptr(kept),
         _ptr(n_kept), _ptr(token_state)))
     return dict(k=k_out, v=v_out, pos=pos_out, kept=kept, n_kept=n_kept)
+
+
+# ---------------------------------------------------------------- serving over the caches
+
+def _attend_outputs(ctx, views, q, o, lse, want):
+    for x in views:
+        if x._torch_dtype != q._torch_dtype or x._device != q._device:
+            raise ValueError("caches and queries must agree in type and device")
+    if q._device.index != ctx.device:
+        raise ValueError(f"the tensors are on {q._device}, the context on device {ctx.device}")
+    if views[-1].n_seq != q._n_seq:
+        raise ValueError(f"cu_rows holds {q._n_seq} sequences, the caches {views[-1].n_seq}")
+    if views[-1].head_dim != q._shape[2]:
+        raise ValueError("queries and keys must have the same width")
+    if o is None:
+        o = torch.empty(q._shape, dtype=q._torch_dtype, device=q._device)
+    elif o.dtype != q._torch_dtype or o.device != q._device or tuple(o.shape) != q._shape or not o.is_contiguous():
+        raise ValueError("o: expected a contiguous tensor of the queries' shape and type")
+    if lse is None and "lse" in want:
+        lse = torch.empty(q._shape[:2], dtype=torch.float32, device=q._device)
+    elif lse is not None and (lse.dtype != torch.float32 or lse.device != q._device or
+                              tuple(lse.shape) != q._shape[:2] or not lse.is_contiguous()):
+        raise ValueError("lse: expected a contiguous float32 tensor [n_rows, Hq]")
+    return o, lse
+
+
+def ckv_attend_window(ctx: Context, kv: BatchView, q: QueryView, *, window: int = 0, n_sink: int = 0, o=None,
+                      lse=None, want=("o",)):
+    """Attention of a ragged batch over its caches: row at position p sees the
+    tokens at positions p - window < p_t <= p and p_t < n_sink (window 0: all up
+    to p).  o [n_rows, Hq, d] of the queries' type; "lse" in ``want`` (or a
+    given ``lse``): float32 [n_rows, Hq]."""
+    o, lse = _attend_outputs(ctx, (kv,), q, o, lse, want)
+    ctx.check(ctx._lib.ckv_attend_window(ctx.handle, ctypes.byref(kv), ctypes.byref(q), int(window), int(n_sink),
+                                         o.data_ptr(), None if lse is None else lse.data_ptr()))
+    return dict(o=o, lse=lse)
+
+
+def ckv_attend_shared(ctx: Context, prefix: BatchView, kv: BatchView, q: QueryView, *, o=None, lse=None,
+                      want=("o",)):
+    """The same over a prefix that every sequence of the batch shares (a view of
+    one sequence, read once for all rows) followed by each sequence's own tokens."""
+    if prefix.n_seq != 1:
+        raise ValueError("prefix: expected a view of one sequence")
+    o, lse = _attend_outputs(ctx, (prefix, kv), q, o, lse, want)
+    ctx.check(ctx._lib.ckv_attend_shared(ctx.handle, ctypes.byref(prefix), ctypes.byref(kv), ctypes.byref(q),
+                                         o.data_ptr(), None if lse is None else lse.data_ptr()))
+    return dict(o=o, lse=lse)
+
+
+def ckv_build_slots(ctx: Context, step: SlotStep):
+    """One step of a batch's block and slot tables.  Returns its outputs:
+    n_tokens, n_free, cu_new, new_row, new_pos, status (device tensors; the
+    tables of ``step`` are updated in place)."""
+    if step._device.index != ctx.device:
+        raise ValueError(f"the tables are on {step._device}, the context on device {ctx.device}")
+    ctx.check(ctx._lib.ckv_build_slots(ctx.handle, ctypes.byref(step)))
+    return step._out
 
 
 # ---------------------------------------------------------------- lifecycle driver

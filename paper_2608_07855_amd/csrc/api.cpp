@@ -1674,3 +1674,196 @@ extern "C" int ckv_select_and_compact(ckv_ctx* c, const ckv_cache_view* in, cons
   CKV_LAUNCH(c, "gather", launch_gather(ga, c->stream));
   return CKV_OK;
 }
+
+// ----------------------------------------------------- serving over the caches
+
+namespace {
+
+bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+  const char *x = static_cast<const char*>(a), *y = static_cast<const char*>(b);
+  return a && b && na && nb && x < y + nb && y < x + na;
+}
+
+// bytes from the first to the last element that a strided tensor of bf16 or
+// fp16 reaches (sizes >= 1, the innermost of d elements)
+size_t span_bytes(int64_t n0, int64_t st0, int64_t n1, int64_t st1, int64_t d) {
+  return (size_t)((n0 - 1) * st0 + (n1 - 1) * st1 + d) * 2;
+}
+
+int check_batch(ckv_ctx* c, const ckv_batch_view* kv, const char* what) {
+  if (!kv || !kv->k || !kv->v || !kv->n_tokens)
+    return fail(c, CKV_ERR_ARG, "%s: the view or one of its pointers is NULL", what);
+  if (kv->dtype != CKV_BF16 && kv->dtype != CKV_F16) return fail(c, CKV_ERR_ARG, "%s: unknown dtype %d", what, kv->dtype);
+  if (kv->head_dim != 64 && kv->head_dim != 128)
+    return fail(c, CKV_ERR_SHAPE, "%s: head_dim %d unsupported (64 or 128)", what, kv->head_dim);
+  if (kv->n_seq < 0 || kv->n_seq > (1 << 20)) return fail(c, CKV_ERR_SHAPE, "%s: n_seq %d out of range", what, kv->n_seq);
+  if (kv->n_kv_heads < 1 || kv->n_kv_heads > 65535) return fail(c, CKV_ERR_SHAPE, "%s: n_kv_heads %d out of range", what, kv->n_kv_heads);
+  if (kv->max_tokens < 0 || kv->max_tokens > INT_MAX - 1024)
+    return fail(c, CKV_ERR_SHAPE, "%s: max_tokens %d out of range", what, kv->max_tokens);
+  if (!aligned16(kv->k) || !aligned16(kv->v) || kv->tok_stride % 8 || kv->head_stride % 8 || (!kv->slot && kv->seq_stride % 8))
+    return fail(c, CKV_ERR_ARG, "%s: K/V rows must be 16-byte aligned (strides multiples of 8)", what);
+  if (kv->tok_stride < kv->head_dim || kv->head_stride < 0 || (!kv->slot && kv->seq_stride < 0))
+    return fail(c, CKV_ERR_SHAPE, "%s: K/V strides too small", what);
+  if (kv->slot && kv->pool_rows < 1) return fail(c, CKV_ERR_SHAPE, "%s: a paged view needs pool_rows >= 1", what);
+  if (kv->n_seq > 1 && ((kv->slot && kv->slot_stride < kv->max_tokens) || (kv->pos && kv->pos_stride < kv->max_tokens)))
+    return fail(c, CKV_ERR_SHAPE, "%s: slot and pos rows must hold max_tokens entries", what);
+  return CKV_OK;
+}
+
+int check_query(ckv_ctx* c, const ckv_query_view* q, const ckv_batch_view* kv, const void* o, const float* lse) {
+  if (!q || !q->cu_rows) return fail(c, CKV_ERR_ARG, "query view or cu_rows is NULL");
+  if (q->n_q_heads < 1 || q->n_q_heads % kv->n_kv_heads)
+    return fail(c, CKV_ERR_SHAPE, "n_q_heads %d is not a multiple of n_kv_heads %d", q->n_q_heads, kv->n_kv_heads);
+  if (q->n_rows < 0 || (int64_t)q->n_rows * q->n_q_heads > INT_MAX - 1024)
+    return fail(c, CKV_ERR_SHAPE, "n_rows %d out of range", q->n_rows);
+  if (q->max_rows < 1) return fail(c, CKV_ERR_SHAPE, "max_rows must be >= 1");
+  if (!std::isfinite(q->scale)) return fail(c, CKV_ERR_ARG, "scale must be finite");
+  if (q->n_rows == 0) return CKV_OK;
+  if (!q->q || !o) return fail(c, CKV_ERR_ARG, "queries or outputs are NULL");
+  if (!aligned16(q->q) || q->row_stride % 8 || q->head_stride % 8 || !aligned16(o))
+    return fail(c, CKV_ERR_ARG, "query and output rows must be 16-byte aligned (strides multiples of 8)");
+  if (q->row_stride < 0 || q->head_stride < 0) return fail(c, CKV_ERR_SHAPE, "query strides must not be negative");
+  const size_t nq = span_bytes(q->n_rows, q->row_stride, q->n_q_heads, q->head_stride, kv->head_dim);
+  const size_t rows = (size_t)q->n_rows * q->n_q_heads, no = rows * kv->head_dim * 2, nl = rows * 4;
+  if (overlap(o, no, q->q, nq) || overlap(lse, nl, q->q, nq) || overlap(o, no, lse, nl))
+    return fail(c, CKV_ERR_ARG, "outputs overlap the queries or each other");
+  return CKV_OK;
+}
+
+SeqCaches make_caches(const ckv_batch_view* v) {
+  SeqCaches c;
+  c.k = v->k;
+  c.v = v->v;
+  c.seq_stride = v->seq_stride;
+  c.head_stride = v->head_stride;
+  c.tok_stride = v->tok_stride;
+  c.slot = v->slot;
+  c.slot_stride = v->slot_stride;
+  c.pos = v->pos;
+  c.pos_stride = v->pos_stride;
+  c.n_tokens = v->n_tokens;
+  c.n_seq = v->n_seq;
+  c.max_tokens = v->max_tokens;
+  c.pool_last = v->slot ? v->pool_rows - 1 : 0;
+  return c;
+}
+
+int attend(ckv_ctx* c, const ckv_batch_view* pre, const ckv_batch_view* kv, const ckv_query_view* q, int32_t window,
+           int32_t n_sink, void* o, float* lse) {
+  if (q->n_rows == 0 || kv->n_seq == 0) return CKV_OK;
+  DeviceGuard g(c->device);
+  if (!g.ok) return fail(c, CKV_ERR_HIP, "cannot select device %d", c->device);
+  AttendArgs a;
+  a.own = make_caches(kv);
+  a.pre = make_caches(pre ? pre : kv);
+  a.has_pre = pre != nullptr;
+  a.f16 = kv->dtype == CKV_F16;
+  a.q = q->q;
+  a.q_row_stride = q->row_stride;
+  a.q_head_stride = q->head_stride;
+  a.cu_rows = q->cu_rows;
+  a.qpos = q->qpos;
+  a.Hq = q->n_q_heads;
+  a.Hkv = kv->n_kv_heads;
+  a.group = a.Hq / a.Hkv;
+  a.D = kv->head_dim;
+  a.n_rows = q->n_rows;
+  a.max_rows = q->max_rows;
+  a.window = window;
+  a.n_sink = n_sink;
+  const float scale = q->scale > 0.f ? q->scale : 1.0f / std::sqrt((float)kv->head_dim);
+  a.sl2 = scale * kLog2eHost;
+  a.o = static_cast<uint16_t*>(o);
+  a.lse = lse;
+  a.nonfinite = c->nf_dev;
+  CKV_LAUNCH(c, "attend", launch_attend_rows(a, c->stream));
+  return CKV_OK;
+}
+
+}  // namespace
+
+extern "C" int ckv_attend_window(ckv_ctx* c, const ckv_batch_view* kv, const ckv_query_view* q, int32_t window,
+                                 int32_t n_sink, void* o, float* lse) {
+  CKV_RANGE("ckv_attend_window");
+  if (!c) return CKV_ERR_ARG;
+  begin_call(c);
+  if (int rc0 = latched_nonfinite(c)) return rc0;
+  int rc;
+  if ((rc = check_batch(c, kv, "caches")) || (rc = check_query(c, q, kv, o, lse))) return rc;
+  if (window < 0 || n_sink < 0) return fail(c, CKV_ERR_ARG, "window %d and n_sink %d must not be negative", window, n_sink);
+  return attend(c, nullptr, kv, q, window, n_sink, o, lse);
+}
+
+extern "C" int ckv_attend_shared(ckv_ctx* c, const ckv_batch_view* prefix, const ckv_batch_view* kv,
+                                 const ckv_query_view* q, void* o, float* lse) {
+  CKV_RANGE("ckv_attend_shared");
+  if (!c) return CKV_ERR_ARG;
+  begin_call(c);
+  if (int rc0 = latched_nonfinite(c)) return rc0;
+  int rc;
+  if ((rc = check_batch(c, prefix, "prefix")) || (rc = check_batch(c, kv, "caches")) || (rc = check_query(c, q, kv, o, lse)))
+    return rc;
+  if (prefix->n_seq != 1) return fail(c, CKV_ERR_SHAPE, "prefix: a view of one sequence is expected, not %d", prefix->n_seq);
+  if (prefix->dtype != kv->dtype || prefix->head_dim != kv->head_dim || prefix->n_kv_heads != kv->n_kv_heads)
+    return fail(c, CKV_ERR_SHAPE, "prefix and caches must agree in type, heads and width");
+  if ((int64_t)prefix->max_tokens + kv->max_tokens > INT_MAX - 1024)
+    return fail(c, CKV_ERR_SHAPE, "prefix and caches hold too many tokens together");
+  return attend(c, prefix, kv, q, 0, 0, o, lse);
+}
+
+extern "C" int ckv_build_slots(ckv_ctx* c, const ckv_slot_step* st) {
+  CKV_RANGE("ckv_build_slots");
+  if (!c) return CKV_ERR_ARG;
+  begin_call(c);
+  if (int rc0 = latched_nonfinite(c)) return rc0;
+  if (!st) return fail(c, CKV_ERR_ARG, "slots: the step is NULL");
+  if (st->n_seq < 0 || st->n_seq > (1 << 20) || st->block_size < 1 || st->n_blocks < 1 || st->max_new < 0 ||
+      (int64_t)st->n_blocks * st->block_size > INT_MAX)
+    return fail(c, CKV_ERR_ARG, "slots: n_seq %d, block_size %d, n_blocks %d or max_new %d out of range", st->n_seq,
+                st->block_size, st->n_blocks, st->max_new);
+  const int64_t n = st->n_seq;
+  if (!st->n_free || !st->free_blocks || !st->n_free_out || !st->cu_new || !st->status ||
+      (n > 0 && (!st->n_tokens || !st->n_new || !st->slot || !st->n_tokens_out)) || (st->max_new > 0 && !st->new_row))
+    return fail(c, CKV_ERR_ARG, "slots: NULL pointer");
+  if (n > 0 && !st->block_table && st->block_size != 1)
+    return fail(c, CKV_ERR_ARG, "slots: block_table may be NULL with block_size 1 only");
+  if (st->slot_stride < 0 || st->block_stride < 0 || st->slot_stride > INT_MAX || st->block_stride > INT_MAX)
+    return fail(c, CKV_ERR_ARG, "slots: table strides out of range");
+  struct Range { const void* p; size_t n; };
+  const size_t word = 4, tab = (size_t)n * st->slot_stride * word, btab = (size_t)n * st->block_stride * word;
+  const Range in[] = {{st->n_tokens, n * word}, {st->n_new, n * word}, {st->next_pos, n * word}, {st->n_free, word}};
+  const Range out[] = {{st->free_blocks, st->n_blocks * word}, {st->block_table, btab}, {st->slot, tab}, {st->pos, tab},
+                       {st->n_tokens_out, n * word}, {st->n_free_out, word}, {st->cu_new, (n + 1) * word},
+                       {st->new_row, st->max_new * word}, {st->new_pos, st->max_new * word}, {st->status, word}};
+  for (size_t i = 0; i < sizeof out / sizeof *out; ++i) {
+    for (const Range& r : in)
+      if (overlap(out[i].p, out[i].n, r.p, r.n)) return fail(c, CKV_ERR_ARG, "slots: an output overlaps an input");
+    for (size_t j = 0; j < i; ++j)
+      if (overlap(out[i].p, out[i].n, out[j].p, out[j].n)) return fail(c, CKV_ERR_ARG, "slots: two outputs overlap");
+  }
+  DeviceGuard g(c->device);
+  if (!g.ok) return fail(c, CKV_ERR_HIP, "cannot select device %d", c->device);
+  SlotArgs a;
+  a.n_seq = st->n_seq;
+  a.block_size = st->block_size;
+  a.n_blocks = st->n_blocks;
+  a.max_new = st->max_new;
+  a.n_tokens = st->n_tokens;
+  a.n_new = st->n_new;
+  a.next_pos = st->next_pos;
+  a.n_free = st->n_free;
+  a.free_blocks = st->free_blocks;
+  a.block_table = st->block_table;
+  a.block_stride = st->block_stride;
+  a.slot = st->slot;
+  a.pos = st->pos;
+  a.slot_stride = st->slot_stride;
+  a.n_tokens_out = st->n_tokens_out;
+  a.n_free_out = st->n_free_out;
+  a.cu_new = st->cu_new;
+  a.new_row = st->new_row;
+  a.new_pos = st->new_pos;
+  a.status = st->status;
+  CKV_LAUNCH(c, "slots", launch_slots(a, c->stream));
+  return CKV_OK;
+}

@@ -371,4 +371,47 @@ hipError_t launch_gather(const GatherArgs& g, hipStream_t s);
 hipError_t launch_pool(const float* score, float* out, int64_t stride, const int32_t* n_tokens, int n_seq,
                        int max_tokens, int kernel, int mode, hipStream_t s);
 
+// ------------------------------------------------- serving over the caches
+
+// resident caches of the sequences of a batch (ckv_batch_view)
+struct SeqCaches {
+  const uint16_t* k;
+  const uint16_t* v;
+  int64_t seq_stride, head_stride, tok_stride;   // elements
+  const int32_t* slot;    // [n_seq][slot_stride] pool rows, or null
+  int64_t slot_stride;
+  const int32_t* pos;     // [n_seq][pos_stride], or null: position of token t = base + t
+  int64_t pos_stride;
+  const int32_t* n_tokens;
+  int n_seq, max_tokens;
+  int pool_last;          // last row of the pool
+};
+
+struct AttendArgs {
+  SeqCaches own, pre;     // pre: the shared tokens (one sequence), when has_pre
+  bool has_pre;
+  bool f16;               // element type
+  const uint16_t* q;
+  int64_t q_row_stride, q_head_stride;
+  const int32_t* cu_rows;
+  const int32_t* qpos;    // or null
+  int Hq, Hkv, group, D;
+  int n_rows, max_rows;
+  int window, n_sink;
+  float sl2;              // softmax scale * log2(e)
+  uint16_t* o;            // [n_rows][Hq][D]
+  float* lse;             // [n_rows][Hq], or null
+  uint32_t* nonfinite;
+};
+hipError_t launch_attend_rows(const AttendArgs& a, hipStream_t s);
+
+struct SlotArgs {
+  int n_seq, block_size, n_blocks, max_new;
+  const int32_t *n_tokens, *n_new, *next_pos, *n_free;
+  int32_t *free_blocks, *block_table, *slot, *pos;
+  int64_t block_stride, slot_stride;
+  int32_t *n_tokens_out, *n_free_out, *cu_new, *new_row, *new_pos, *status;
+};
+hipError_t launch_slots(const SlotArgs& a, hipStream_t s);
+
 }  // namespace ckv
