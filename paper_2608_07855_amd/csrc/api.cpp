@@ -41,6 +41,8 @@ constexpr int kMaxSplitTokens = 8192;
 // whole of a 40-layer commit; a 65536-token layer (45 MB) fills the device by
 // itself, and 8 share a launch.
 constexpr size_t kBatchBytes = size_t(384) << 20;
+// arrival counts of the attention calls, one int for every split
+constexpr size_t kAttendCounts = size_t(1) << 18;
 // the token-mass kernel (126 registers, 40 KB of LDS) keeps two workgroups per
 // compute unit busy: 512 token chunks measured 31.7 us against 35.3 us with 256
 constexpr int kMassBlocks = 512;
@@ -91,6 +93,11 @@ struct ckv_ctx {
   // single calls have been recorded with (a captured graph of them).
   struct Arena { char* p = nullptr; size_t cap = 0; };
   Arena ws, batch_ws;
+  // Split partials and arrival counts of the attention calls.  Captured graphs
+  // refer to it, so what it outgrows is kept until the context goes.
+  Arena attend_ws;
+  std::vector<Arena> outgrown;
+  size_t outgrown_bytes = 0;
   size_t ws_limit = 0;   // of both together
   std::string err;
   PinnedSlot slots[kPinnedSlots];
@@ -251,6 +258,44 @@ int ensure_batch_ws(ckv_ctx* c, size_t need) {
   release(c->batch_ws);
   if (allocate(c->batch_ws, want) || (want > need && allocate(c->batch_ws, need))) return CKV_OK;
   return fail(c, CKV_ERR_NOMEM, "hipMalloc of %zu workspace bytes failed", need);
+}
+
+// Room for the attention calls: arrival counts (zero between calls) in the
+// first kAttendCounts bytes, split partials behind them.  *room is false where
+// the workspace limit leaves none.  No stream is waited for: what is outgrown
+// stays where it is, for work under way and for captured graphs.
+int ensure_attend_ws(ckv_ctx* c, size_t counts, size_t part, bool* room) {
+  const size_t need = kAttendCounts + part;
+  *room = counts <= kAttendCounts;
+  if (!*room || need <= c->attend_ws.cap) return CKV_OK;
+  const size_t held = c->ws.cap + c->batch_ws.cap + c->attend_ws.cap + c->outgrown_bytes;
+  size_t want = std::max(need, 2 * c->attend_ws.cap);
+  if (c->ws_limit) {
+    const size_t left = c->ws_limit - std::min(c->ws_limit, held);
+    *room = need <= left;
+    if (!*room) return CKV_OK;
+    want = std::min(want, left);
+  }
+  hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
+  CKV_HIP(c, hipStreamIsCapturing(c->stream, &st));
+  if (st != hipStreamCaptureStatusNone)
+    return fail(c, CKV_ERR_NOMEM, "the workspace has to grow to %zu bytes, which a capture cannot record: make an equal call before it", need);
+  ckv_ctx::Arena a;
+  if (!allocate(a, want) && !allocate(a, need)) return fail(c, CKV_ERR_NOMEM, "hipMalloc of %zu workspace bytes failed", need);
+  const hipError_t e = hipMemsetAsync(a.p, 0, kAttendCounts, c->stream);
+  if (e != hipSuccess) {
+    release(a);
+    return hip_fail(c, e, "hipMemsetAsync of the arrival counts");
+  }
+  try {
+    if (c->attend_ws.p) c->outgrown.push_back(c->attend_ws);
+  } catch (const std::bad_alloc&) {
+    release(a);
+    return fail(c, CKV_ERR_NOMEM, "out of host memory");
+  }
+  c->outgrown_bytes += c->attend_ws.cap;
+  c->attend_ws = a;
+  return CKV_OK;
 }
 
 void place(Plan& plan, char* base) {
@@ -586,6 +631,8 @@ extern "C" int ckv_destroy(ckv_ctx* c) {
     (void)hipStreamSynchronize(c->stream);
     release(c->ws);
     release(c->batch_ws);
+    release(c->attend_ws);
+    for (auto& a : c->outgrown) release(a);
     if (c->sel_ctrl) (void)hipFree(c->sel_ctrl);
     if (c->sel_hist) (void)hipFree(c->sel_hist);
     for (auto& e : c->pages)
@@ -643,7 +690,7 @@ extern "C" int ckv_set_workspace_limit(ckv_ctx* c, size_t bytes) {
   return CKV_OK;
 }
 
-extern "C" size_t ckv_workspace_bytes(const ckv_ctx* c) { return c ? c->ws.cap + c->batch_ws.cap : 0; }
+extern "C" size_t ckv_workspace_bytes(const ckv_ctx* c) { return c ? c->ws.cap + c->batch_ws.cap + c->attend_ws.cap + c->outgrown_bytes : 0; }
 
 extern "C" int ckv_set_policy(ckv_ctx* c, uint32_t flags) {
   if (!c) return CKV_ERR_ARG;
@@ -1776,7 +1823,25 @@ int attend(ckv_ctx* c, const ckv_batch_view* pre, const ckv_batch_view* kv, cons
   a.o = static_cast<uint16_t*>(o);
   a.lse = lse;
   a.nonfinite = c->nf_dev;
-  CKV_LAUNCH(c, "attend", launch_attend_rows(a, c->stream));
+  if (pre) {
+    CKV_LAUNCH(c, "attend", launch_attend_rows(a, c->stream));
+    return CKV_OK;
+  }
+  NarrowPlan p = plan_narrow(a, kv->max_tokens, true);
+  float* part = nullptr;
+  int* arrive = nullptr;
+  if (p.split) {
+    const size_t counts = round_up(p.items * sizeof(int), kAlign);
+    bool room;
+    if (int rc = ensure_attend_ws(c, counts, (size_t)p.items * 16 * (a.D + 2) * sizeof(float), &room)) return rc;
+    if (room) {
+      arrive = reinterpret_cast<int*>(c->attend_ws.p);
+      part = reinterpret_cast<float*>(c->attend_ws.p + kAttendCounts);
+    } else {
+      p = plan_narrow(a, kv->max_tokens, false);
+    }
+  }
+  CKV_LAUNCH(c, "attend", launch_attend_narrow(a, p, part, arrive, c->stream));
   return CKV_OK;
 }
 

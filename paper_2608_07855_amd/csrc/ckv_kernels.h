@@ -405,6 +405,17 @@ struct AttendArgs {
 };
 hipError_t launch_attend_rows(const AttendArgs& a, hipStream_t s);
 
+// Launch of the few-rows kernel: its grid, and the split partials that it needs
+// ([items][16 rows][D + 2] floats, and one zeroed int an item) when `split`.
+struct NarrowPlan {
+  int64_t items;
+  int target, min_chunk;
+  bool split;
+};
+// room: whether there may be a workspace at all
+NarrowPlan plan_narrow(const AttendArgs& a, int64_t max_tokens, bool room);
+hipError_t launch_attend_narrow(const AttendArgs& a, const NarrowPlan& p, float* part, int* arrive, hipStream_t s);
+
 struct SlotArgs {
   int n_seq, block_size, n_blocks, max_new;
   const int32_t *n_tokens, *n_new, *next_pos, *n_free;
