@@ -5,53 +5,35 @@
 //   x_t = scale q.k_t over the tokens with p_t <= p and (no window, or
 //   p - p_t < window, or p_t < n_sink);  lse = log sum e^x;  o = sum e^(x - lse) v.
 // Logits are carried in log2 units (scale * log2(e)).
-#include "ckv_device.h"
-#include "ckv_kernels.h"
+#include "attend_device.h"
 
 #include <algorithm>
-#include <climits>
 
 namespace ckv {
 
 namespace {
 
-__device__ __forceinline__ int clampi(int x, int lo, int hi) { return min(max(x, lo), hi); }
-
-__device__ __forceinline__ int seq_tokens(const SeqCaches& c, int s) { return clampi(c.n_tokens[s], 0, c.max_tokens); }
-
-__device__ __forceinline__ int row_start(const AttendArgs& a, int s) { return clampi(a.cu_rows[s], 0, a.n_rows); }
-
-// the sequence that owns row r, or -1: the last s with cu_rows[s] <= r
-__device__ __forceinline__ int row_seq(const AttendArgs& a, int r) {
-  int lo = 0, hi = a.own.n_seq;            // cu_rows[lo] <= r < cu_rows[hi], once both are checked
-  if (row_start(a, 0) > r || row_start(a, hi) <= r) return -1;
-  while (hi - lo > 1) {
-    const int m = (lo + hi) >> 1;
-    if (row_start(a, m) <= r) lo = m;
-    else hi = m;
-  }
-  return lo;
-}
-
-__device__ __forceinline__ bool sees(int p, int qp, int window, int n_sink) {
-  return p <= qp && (window == 0 || (uint32_t)qp - (uint32_t)p < (uint32_t)window || p < n_sink);
-}
-
 template <bool F16>
-__device__ __forceinline__ float elem(uint32_t bits) {
-  if constexpr (F16) return (float)__builtin_bit_cast(_Float16, (uint16_t)bits);
-  else return bf16_bits_to_float(bits);
+__device__ __forceinline__ f32x4 mfma16(u32x4 x, u32x4 y, f32x4 c) {
+  if constexpr (F16)
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, x), __builtin_bit_cast(f16x8, y), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), c, 0, 0, 0);
 }
 
-// round to nearest even, NaN stays NaN
-template <bool F16>
-__device__ __forceinline__ uint16_t to_elem(float x) {
-  if constexpr (F16) return __builtin_bit_cast(uint16_t, (_Float16)x);
-  else return __builtin_bit_cast(uint16_t, (__bf16)x);
+// over the four 16-lane rows of a wave: lanes l, l ^ 16, l ^ 32, l ^ 48
+__device__ __forceinline__ float max_rows16(float v) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return max32(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ __forceinline__ float sum_rows16(float v) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return sum32(__uint_as_float(r[0]) + __uint_as_float(r[1]));
 }
 
-// One wave per (row, query head): 64 tokens at a time, one per lane; then
-// every lane adds their weighted values into its own widths.
+// Without a workspace for partial sums (a workspace limit): one wave per (row,
+// query head), 64 tokens at a time, one per lane; then every lane adds their
+// weighted values into its own widths.
 template <int D, bool F16>
 __global__ __launch_bounds__(256) void attend_rows_kernel(AttendArgs a) {
   const int lane = threadIdx.x & 63;
@@ -62,14 +44,8 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(AttendArgs a) {
   if (s < 0) return;
   const int g = h / a.group;
   const int n = seq_tokens(a.own, s), base = a.has_pre ? seq_tokens(a.pre, 0) : 0;
-  int qp;
-  if (a.qpos) {
-    qp = a.qpos[r];
-  } else {
-    const int t = n - (row_start(a, s + 1) - r);
-    if (!a.own.pos) qp = base + t;
-    else qp = t >= 0 ? a.own.pos[s * a.own.pos_stride + t] : INT_MIN;
-  }
+  const int r0 = row_start(a, s);
+  const int qp = row_position(a, s, r0, row_start(a, s + 1) - r0, r - r0, n, base);
   const uint16_t* q = a.q + r * a.q_row_stride + h * a.q_head_stride;
   constexpr int PW = D / 64;
   float m = -INFINITY, l = 0.f, acc[PW] = {};
@@ -130,264 +106,6 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(AttendArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// Work items.  A sequence's query rows of one KV head (position by position,
-// the head's group of query heads innermost) are cut into blocks, and the
-// tokens that a block sees into splits of about `chunk` tokens, so that few
-// rows behind a long cache still fill the device.  Lengths are known on the
-// device only: every workgroup forms the batch's sums itself (two loads and a
-// reduction for up to a workgroup's threads of sequences) instead of waiting
-// for a planning launch, and the grid is the host's bound of their number.
-// ---------------------------------------------------------------------------
-struct Item {
-  int s;            // sequence, -1: no such item
-  int rb;           // row block
-  int split, n_split;
-  int64_t e;        // number of the item among those of its KV head
-};
-
-// tokens that a block of rows of sequence s sees, as far as the lengths tell:
-// decides how many splits it gets, not what they hold
-__device__ __forceinline__ int seen_estimate(const AttendArgs& a, int n, int block_rows) {
-  if (a.window == 0) return n;
-  const long long w = (long long)a.window + a.n_sink + block_rows / a.group + 1;
-  return (int)min((long long)n, w);
-}
-
-template <int NT>
-__device__ __forceinline__ long long block_sum(long long v, long long* sh) {
-  const int tid = threadIdx.x;
-#pragma unroll
-  for (int off = 32; off; off >>= 1) v += __shfl_xor(v, off, 64);
-  __syncthreads();
-  if ((tid & 63) == 0) sh[tid >> 6] = v;
-  __syncthreads();
-  long long t = 0;
-#pragma unroll
-  for (int w = 0; w < NT / 64; ++w) t += sh[w];
-  return t;
-}
-
-struct ItemShared {
-  long long wave[16];
-  int found[4];
-};
-
-// Item e of a KV head: blocks of RB rows, about `target` items over all heads, at least min_chunk tokens each.
-template <int NT, int RB>
-__device__ Item find_item(const AttendArgs& a, int64_t e, int target, int min_chunk, ItemShared& sh) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n_seq = a.own.n_seq;
-  auto load = [&](int s, int& nrb, int& est) {
-    nrb = est = 0;
-    if (s < n_seq) {
-      const int r0 = row_start(a, s), R = max(row_start(a, s + 1) - r0, 0);
-      nrb = (int)(((int64_t)R * a.group + RB - 1) / RB);
-      est = seen_estimate(a, seq_tokens(a.own, s), min(RB, R * a.group));
-    }
-  };
-  int nrb, est;
-  load(tid, nrb, est);
-  long long work = (long long)nrb * est;
-  for (int s = tid + NT; s < n_seq; s += NT) {
-    int b, t;
-    load(s, b, t);
-    work += (long long)b * t;
-  }
-  work = block_sum<NT>(work, sh.wave) * a.Hkv;
-  const int64_t chunk = max((int64_t)min_chunk, (work + target - 1) / target);
-  if (tid == 0) sh.found[0] = -1;
-  int64_t before = 0;
-  for (int s0 = 0; s0 < n_seq; s0 += NT) {
-    if (s0) load(s0 + tid, nrb, est);
-    const int n_split = est > 0 ? (int)((est + chunk - 1) / chunk) : 1;
-    const long long mine = (long long)nrb * n_split;
-    long long v = mine;
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-      const long long u = __shfl_up(v, off, 64);
-      if (lane >= off) v += u;
-    }
-    __syncthreads();
-    if (lane == 63) sh.wave[wave] = v;
-    __syncthreads();
-    long long total = 0;
-#pragma unroll
-    for (int w = 0; w < NT / 64; ++w) {
-      if (w < wave) v += sh.wave[w];
-      total += sh.wave[w];
-    }
-    const int64_t at = e - before - (v - mine);
-    if (at >= 0 && at < mine) {
-      sh.found[0] = s0 + tid;
-      sh.found[1] = (int)(at / n_split);
-      sh.found[2] = (int)(at % n_split);
-      sh.found[3] = n_split;
-    }
-    before += total;
-    if (before > e) break;
-  }
-  __syncthreads();
-  Item it;
-  it.s = __builtin_amdgcn_readfirstlane(sh.found[0]);
-  it.rb = __builtin_amdgcn_readfirstlane(sh.found[1]);
-  it.split = __builtin_amdgcn_readfirstlane(sh.found[2]);
-  it.n_split = __builtin_amdgcn_readfirstlane(sh.found[3]);
-  it.e = e;
-  return it;
-}
-
-// First t of [0, n) with pos[t] > key (n if none), pos ascending: a wave
-// tries 64 places at once, so 131072 positions take three dependent loads.
-__device__ __forceinline__ int upper_bound(const int32_t* pos, int n, long long key) {
-  const int lane = threadIdx.x & 63;
-  int lo = 0, len = n;
-  while (len > 0) {
-    const int step = (len + 63) / 64;
-    const int t = lo + min(lane * step + step - 1, len - 1);     // last place of the lane's part
-    const bool le = pos[t] <= key && lane * step < len;
-    const int parts = __popcll(__ballot(le));                    // parts that lie at or below the key
-    const int skip = min(parts * step, len);
-    lo += skip;
-    len = min(step - 1, len - skip);
-  }
-  return lo;
-}
-
-// The tokens that rows at positions qmin..qmax see between them, as one range
-// of indexes u < cnt: first tokens t = u < ns, then t = u + shift.
-struct Range {
-  int ns, shift, cnt;
-  __device__ __forceinline__ int token(int u) const { return u < ns ? u : u + shift; }
-};
-
-__device__ __forceinline__ Range seen_range(const SeqCaches& c, int sq, int n, int base, int qmin, int qmax, int window,
-                                            int n_sink) {
-  int hi, lo = 0, ns = 0;
-  if (c.pos) {
-    const int32_t* p = c.pos + sq * c.pos_stride;
-    hi = upper_bound(p, n, qmax);
-    if (window) {
-      lo = upper_bound(p, n, (long long)qmin - window);
-      if (n_sink) ns = upper_bound(p, n, (long long)n_sink - 1);
-    }
-  } else {
-    auto in = [&](long long t) { return (int)min(max(t, 0ll), (long long)n); };
-    hi = in((long long)qmax + 1 - base);
-    if (window) {
-      lo = in((long long)qmin - window + 1 - base);
-      ns = in((long long)n_sink - base);
-    }
-  }
-  lo = min(lo, hi);
-  ns = min(ns, hi);
-  Range r;
-  if (lo <= ns) {
-    r.ns = 0;
-    r.shift = 0;
-    r.cnt = hi;
-  } else {
-    r.ns = ns;
-    r.shift = lo - ns;
-    r.cnt = ns + hi - lo;
-  }
-  return r;
-}
-
-// Position of row p of the R rows of sequence s, whose first row is r0.
-__device__ __forceinline__ int row_position(const AttendArgs& a, int s, int r0, int R, int p, int n, int base) {
-  if (a.qpos) return a.qpos[r0 + p];
-  const int t = n - R + p;
-  if (!a.own.pos) return base + t;
-  return t >= 0 ? a.own.pos[s * a.own.pos_stride + t] : INT_MIN;
-}
-
-// ---------------------------------------------------------------------------
-// Loads from global memory straight into LDS: lane l's 16 (or 4) bytes land at
-// base + 16 l (4 l), with the base the same for the whole wave.  No register
-// waits for them; the wave counts them itself (vmcnt, in order).
-// ---------------------------------------------------------------------------
-__device__ __forceinline__ uint32_t lds_at(const void* p) {
-  return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
-}
-__device__ __forceinline__ void load_lds16(const void* g, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(g) : "memory");
-}
-__device__ __forceinline__ void load_lds4(const void* g, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(g) : "memory");
-}
-// until at most N of the wave's own global loads and stores are under way
-template <int N>
-__device__ __forceinline__ void wait_loads() {
-  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
-}
-// until the wave's LDS reads have returned (before their place is loaded again)
-__device__ __forceinline__ void wait_lds_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
-
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef short s16x8 __attribute__((ext_vector_type(8)));
-// 64 bits of each lane, transposed inside each 16 lanes: lane i gets element
-// i % 4 of lanes 4e + i / 4, e = 0..3
-__device__ __forceinline__ s16x4 lds_read_tr(uint32_t at) {
-  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(uintptr_t)at);
-}
-__device__ __forceinline__ u32x4 lds_read16(uint32_t at) {
-  return *(const __attribute__((address_space(3))) u32x4*)(uintptr_t)at;
-}
-
-template <bool F16>
-__device__ __forceinline__ f32x4 mfma16(u32x4 x, u32x4 y, f32x4 c) {
-  if constexpr (F16)
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, x), __builtin_bit_cast(f16x8, y), c, 0, 0, 0);
-  else
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), c, 0, 0, 0);
-}
-
-// over the four 16-lane rows of a wave: lanes l, l ^ 16, l ^ 32, l ^ 48
-__device__ __forceinline__ float max_rows16(float v) {
-  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return max32(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
-}
-__device__ __forceinline__ float sum_rows16(float v) {
-  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return sum32(__uint_as_float(r[0]) + __uint_as_float(r[1]));
-}
-
-// Words that cross workgroups (split partials): agent-scope accesses, which
-// pass the per-XCD L2 caches by.
-__device__ __forceinline__ void put_word(float* p, float v) {
-  __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ float get_word(const float* p) {
-  return __hip_atomic_load(const_cast<float*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-
-// Four widths of a finished row (rr: row of sequence start r0 and KV head g,
-// position by position), weighted values `acc` against the largest logit m
-// (log2 units) with sum l.
-template <int D, bool F16>
-__device__ __forceinline__ void store_row(const AttendArgs& a, int r0, int rr, int g, int w4, f32x4 acc, float m, float l) {
-  const int64_t out = (int64_t)(r0 + rr / a.group) * a.Hq + g * a.group + rr % a.group;
-  const float inv = 1.f / l;
-  uint2 w;
-  bool bad = false;
-  uint16_t y[4];
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const float v = l == 0.f ? 0.f : acc[e] * inv;
-    bad |= !__builtin_isfinite(v);
-    y[e] = to_elem<F16>(v);
-  }
-  w.x = y[0] | (uint32_t)y[1] << 16;
-  w.y = y[2] | (uint32_t)y[3] << 16;
-  *reinterpret_cast<uint2*>(a.o + out * D + w4) = w;
-  if (w4 == 0) {
-    const float lse = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
-    bad |= l != 0.f && !__builtin_isfinite(lse);
-    if (a.lse) a.lse[out] = lse;
-  }
-  if (bad) latch_nonfinite(a.nonfinite);
-}
-
-// ---------------------------------------------------------------------------
 // Few rows: a wave takes 16 query rows and its own tokens, 32 at a time.
 //
 // S^T = K Q^T and O^T += V^T P^T on v_mfma_f32_16x16x32: a score block has its
@@ -427,14 +145,8 @@ struct Narrow {
   __device__ static constexpr int row(int r) { return LANES * (r % LOADS) + r / LOADS; }
 };
 
-struct SplitSpace {
-  float* o;        // [items][rows of a block][D], weighted values against m
-  float* ml;       // [items][rows of a block][2]: largest logit (log2 units), sum
-  int* arrive;     // [items], zero between calls
-};
-
 template <int D, bool F16, bool TAB>
-__global__ __launch_bounds__(Narrow<D>::NT) void attend_narrow_kernel(AttendArgs a, SplitSpace sp, int target, int min_chunk) {
+__global__ __launch_bounds__(Narrow<D>::NT) void attend_narrow_kernel(AttendArgs a, SplitSpace sp, int target, int min_chunk, PrefixParts pp) {
   using L = Narrow<D>;
   constexpr int NT = L::NT, NW = L::NW;
   __shared__ __align__(16) char tiles[NW * L::kWaveB];
@@ -681,6 +393,11 @@ __global__ __launch_bounds__(Narrow<D>::NT) void attend_narrow_kernel(AttendArgs
     sl[wave][c] = l;
   }
   __syncthreads();
+  auto finish = [&](int row, int w4, Joined j) {
+    const int rr = it.rb * L::kRows + row;
+    if (pp.n_split) add_prefix(a, pp, D, (r0 - row_start(a, 0)) * a.group + rr, g, w4, j);
+    store_row<D, F16>(a, r0, rr, g, w4, j.acc, j.m, j.l);
+  };
   constexpr int TPR = D / 4;                 // threads of a row, four widths each
   const int64_t item = blockIdx.x;
   for (int i = tid; i < n_rows * TPR; i += NT) {
@@ -698,7 +415,7 @@ __global__ __launch_bounds__(Narrow<D>::NT) void attend_narrow_kernel(AttendArgs
       acc += *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(tiles + w * L::kWaveB) + row * OP + w4) * f;
     }
     if (it.n_split == 1) {
-      store_row<D, F16>(a, r0, it.rb * L::kRows + row, g, w4, acc, mm, ll);
+      finish(row, w4, Joined{mm, ll, acc});
     } else {
       float* po = sp.o + (item * L::kRows + row) * D + w4;
 #pragma unroll
@@ -723,21 +440,16 @@ __global__ __launch_bounds__(Narrow<D>::NT) void attend_narrow_kernel(AttendArgs
   if (!last) return;
   for (int i = tid; i < n_rows * TPR; i += NT) {
     const int row = i / TPR, w4 = (i % TPR) * 4;
-    float mm = -INFINITY, ll = 0.f;
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    Joined all = {-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f}};
     for (int j = 0; j < it.n_split; ++j) {
       const int64_t at = (first + (int64_t)j * a.Hkv) * L::kRows + row;
       const float pm = get_word(sp.ml + at * 2), pl = get_word(sp.ml + at * 2 + 1);
       f32x4 po;
 #pragma unroll
       for (int e = 0; e < 4; ++e) po[e] = get_word(sp.o + at * D + w4 + e);
-      const float nm = fmaxf(mm, pm), ref = nm == -INFINITY ? 0.f : nm;
-      const float f0 = __builtin_amdgcn_exp2f(mm - ref), f1 = __builtin_amdgcn_exp2f(pm - ref);
-      ll = ll * f0 + pl * f1;
-      acc = acc * f0 + po * f1;
-      mm = nm;
+      all.add(pm, pl, po);
     }
-    store_row<D, F16>(a, r0, it.rb * L::kRows + row, g, w4, acc, mm, ll);
+    finish(row, w4, all);
   }
 }
 
@@ -756,8 +468,9 @@ hipError_t launch_attend_rows(const AttendArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-NarrowPlan plan_narrow(const AttendArgs& a, int64_t max_tokens, bool room) {
-  NarrowPlan p;
+AttendPlan plan_narrow(const AttendArgs& a, int64_t max_tokens, bool room) {
+  AttendPlan p;
+  p.rows = 16;
   const int64_t n_seq = std::min(a.own.n_seq, a.n_rows);
   const int64_t blocks = (int64_t)a.n_rows * a.group / 16 + n_seq;      // row blocks of a KV head, at most
   const int64_t slots = 2 * 256;                                        // workgroups that run at once
@@ -773,14 +486,11 @@ NarrowPlan plan_narrow(const AttendArgs& a, int64_t max_tokens, bool room) {
   return p;
 }
 
-hipError_t launch_attend_narrow(const AttendArgs& a, const NarrowPlan& p, float* part, int* arrive, hipStream_t s) {
-  SplitSpace sp;
-  sp.o = part;
-  sp.ml = part + p.items * 16 * a.D;
-  sp.arrive = arrive;
+hipError_t launch_attend_narrow(const AttendArgs& a, const AttendPlan& p, const SplitSpace& sp, const PrefixParts& pp,
+                                hipStream_t s) {
   const dim3 grid((unsigned)p.items);
   const bool tab = a.own.slot || a.own.pos;
-#define CKV_NARROW(D, F16, TAB) attend_narrow_kernel<D, F16, TAB><<<grid, Narrow<D>::NT, 0, s>>>(a, sp, p.target, p.min_chunk)
+#define CKV_NARROW(D, F16, TAB) attend_narrow_kernel<D, F16, TAB><<<grid, Narrow<D>::NT, 0, s>>>(a, sp, p.target, p.min_chunk, pp)
 #define CKV_NARROW2(D, F16) \
   if (tab) CKV_NARROW(D, F16, true); \
   else CKV_NARROW(D, F16, false)

@@ -405,16 +405,44 @@ struct AttendArgs {
 };
 hipError_t launch_attend_rows(const AttendArgs& a, hipStream_t s);
 
-// Launch of the few-rows kernel: its grid, and the split partials that it needs
-// ([items][16 rows][D + 2] floats, and one zeroed int an item) when `split`.
-struct NarrowPlan {
+// Split partials: item by item, a row block's rows each.
+struct SplitSpace {
+  float* o;        // [items][rows][D], weighted values against the largest logit
+  float* ml;       // [items][rows][2]: that logit (log2 units), the sum of the weights
+  int* arrive;     // few-rows kernel: [items], zero between calls
+};
+
+// Partial sums over the shared tokens by packed row (all sequences' rows of a
+// KV head, position by position): block, split, KV head, row.
+struct PrefixParts {
+  const float* o;
+  const float* ml;
+  int n_split, block_rows;   // n_split 0: none
+};
+
+// How a call is cut into items (row blocks of `rows` rows and splits); room:
+// whether there may be partial sums.  split: whether there are.
+struct AttendPlan {
   int64_t items;
-  int target, min_chunk;
+  int rows, target, min_chunk;
   bool split;
 };
-// room: whether there may be a workspace at all
-NarrowPlan plan_narrow(const AttendArgs& a, int64_t max_tokens, bool room);
-hipError_t launch_attend_narrow(const AttendArgs& a, const NarrowPlan& p, float* part, int* arrive, hipStream_t s);
+AttendPlan plan_narrow(const AttendArgs& a, int64_t max_tokens, bool room);
+AttendPlan plan_wide(const AttendArgs& a, int64_t max_tokens, bool room);
+struct PrefixPlan {
+  int64_t blocks;
+  int rows, n_split;
+};
+PrefixPlan plan_prefix(const AttendArgs& a);
+
+// Few rows: finished in one launch (with the prefix's partial sums joined).
+hipError_t launch_attend_narrow(const AttendArgs& a, const AttendPlan& p, const SplitSpace& sp, const PrefixParts& pp,
+                                hipStream_t s);
+// Many rows: what is split or shares a prefix is finished by launch_attend_join.
+hipError_t launch_attend_wide(const AttendArgs& a, const AttendPlan& p, const SplitSpace& sp, hipStream_t s);
+hipError_t launch_attend_prefix(const AttendArgs& a, const PrefixPlan& p, const SplitSpace& sp, hipStream_t s);
+hipError_t launch_attend_join(const AttendArgs& a, const AttendPlan& p, const SplitSpace& sp, const PrefixParts& pp,
+                              hipStream_t s);
 
 struct SlotArgs {
   int n_seq, block_size, n_blocks, max_new;
