@@ -240,15 +240,21 @@ __device__ __forceinline__ void wait_loads() {
 // until the wave's LDS reads have returned (before their place is loaded again)
 __device__ __forceinline__ void wait_lds_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
+typedef __attribute__((address_space(3))) char lds_char;
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 // 64 bits of each lane, transposed inside each 16 lanes: lane i gets element
 // i % 4 of lanes 4e + i / 4, e = 0..3
-__device__ __forceinline__ s16x4 lds_read_tr(uint32_t at) {
-  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(uintptr_t)at);
+__device__ __forceinline__ s16x4 lds_read_tr(uint32_t at, int plus = 0) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)((const lds_char*)(uintptr_t)at + plus));
 }
-__device__ __forceinline__ u32x4 lds_read16(uint32_t at) {
-  return *(const __attribute__((address_space(3))) u32x4*)(uintptr_t)at;
+__device__ __forceinline__ u32x4 lds_read16(uint32_t at, int plus = 0) {
+  return *(const __attribute__((address_space(3))) u32x4*)((const lds_char*)(uintptr_t)at + plus);
+}
+
+// largest of three in one instruction (v_maximum3_f32; NaN if one of them is)
+__device__ __forceinline__ float max3(float x, float y, float z) {
+  return __builtin_elementwise_maximum(__builtin_elementwise_maximum(x, y), z);
 }
 
 // Words that cross workgroups (split partials): agent-scope accesses, which

@@ -23,6 +23,7 @@ namespace {
 // in either type, sums are float32), so that the output is rarely rescaled.
 // ---------------------------------------------------------------------------
 constexpr float kLag = 8.f;   // log2 units
+constexpr int kAhead = 4;     // operands read from LDS ahead of their products
 
 template <int D, int RW, int NW>
 struct Wide {
@@ -30,8 +31,7 @@ struct Wide {
   static constexpr int CH = D / 8, LANES = 64 / CH;
   static constexpr int LOADS = kTok / LANES / NW;      // loads of a wave for a tile of K (or V)
   static constexpr int kRowB = 2 * D, kTileB = kTok * kRowB;
-  static constexpr int NBUF = 3;
-  static constexpr int kLds = NBUF * 2 * kTileB + NW * 4 * 256;
+  static constexpr int kLds = 6 * kTileB + NW * 4 * 256;   // three tiles of K, three of V, four tables a wave
 };
 
 template <bool F16>
@@ -145,7 +145,7 @@ __global__ __launch_bounds__(64 * NW) void attend_wide_kernel(AttendArgs a, Spli
   const int per_split = (n_tiles + splits - 1) / splits;
   const int tile0 = min(split * per_split, n_tiles), tile1 = min(tile0 + per_split, n_tiles);
 
-  const uint32_t lds = lds_at(tiles), tab = lds + L::NBUF * 2 * L::kTileB + wave * 4 * 256;
+  const uint32_t lds = lds_at(tiles), tab = lds + 6 * L::kTileB + wave * 4 * 256;
   const int grp = lane / L::CH, ch = lane % L::CH;
   constexpr int kOwn = L::LOADS * L::LANES;               // tokens of a tile that the wave loads
   const int64_t head = g * kv.head_stride + (kv.slot ? 0 : s * kv.seq_stride);
@@ -158,25 +158,39 @@ __global__ __launch_bounds__(64 * NW) void attend_wide_kernel(AttendArgs a, Spli
   auto load_tables = [&](int tile) {
     if constexpr (TAB) load_lds4(slots + token(tile, wave * kOwn + lane % kOwn), tab + (tile & 3) * 256);
   };
-  auto load_tile = [&](int tile) {
-    const uint32_t kb = lds + (tile % L::NBUF) * 2 * L::kTileB, vb = kb + L::kTileB;
-    int rows[L::LOADS];
-#pragma unroll
-    for (int i = 0; i < L::LOADS; ++i) {
-      if constexpr (TAB) {
-        const auto* w = (const __attribute__((address_space(3))) int*)(uintptr_t)(tab + (tile & 3) * 256);
-        rows[i] = (int)min((uint32_t)w[i * L::LANES + grp], (uint32_t)kv.pool_last);
-      } else {
-        rows[i] = token(tile, wave * kOwn + i * L::LANES + grp);
-      }
+  // K of tile kt and V of tile vt travel together (V is needed one step later)
+  auto row_offset = [&](int tile, int i) -> int64_t {
+    int row;
+    if constexpr (TAB) {
+      const auto* w = (const __attribute__((address_space(3))) int*)(uintptr_t)(tab + (tile & 3) * 256);
+      row = (int)min((uint32_t)w[i * L::LANES + grp], (uint32_t)kv.pool_last);
+    } else {
+      row = token(tile, wave * kOwn + i * L::LANES + grp);
     }
+    return row * row_bytes;
+  };
+  auto load_k = [&](int tile) {
+    const uint32_t kb = lds + (tile % 3) * L::kTileB;
+    int64_t at[L::LOADS];
+#pragma unroll
+    for (int i = 0; i < L::LOADS; ++i) at[i] = row_offset(tile, i);
     wait_lds_reads();
 #pragma unroll
     for (int i = 0; i < L::LOADS; ++i) {
       const int r = wave * kOwn + i * L::LANES + grp;
-      const int64_t at = rows[i] * row_bytes;
-      load_lds16(kh + at + ((ch ^ (r & (L::CH - 1))) << 4), kb + (wave * L::LOADS + i) * 1024);
-      load_lds16(vh + at + ((ch ^ (2 * r & (L::CH - 1))) << 4), vb + (wave * L::LOADS + i) * 1024);
+      load_lds16(kh + at[i] + ((ch ^ (r & (L::CH - 1))) << 4), kb + (wave * L::LOADS + i) * 1024);
+    }
+  };
+  auto load_v = [&](int tile) {
+    const uint32_t vb = lds + (3 + tile % 3) * L::kTileB;
+    int64_t at[L::LOADS];
+#pragma unroll
+    for (int i = 0; i < L::LOADS; ++i) at[i] = row_offset(tile, i);
+    wait_lds_reads();
+#pragma unroll
+    for (int i = 0; i < L::LOADS; ++i) {
+      const int r = wave * kOwn + i * L::LANES + grp;
+      load_lds16(vh + at[i] + ((ch ^ (2 * r & (L::CH - 1))) << 4), vb + (wave * L::LOADS + i) * 1024);
     }
   };
 
@@ -191,85 +205,148 @@ __global__ __launch_bounds__(64 * NW) void attend_wide_kernel(AttendArgs a, Spli
   }
   bool hidden = false;          // some tile held tokens that not all rows see
 
-  auto compute = [&](int tile) {
-    const uint32_t kb = lds + (tile % L::NBUF) * 2 * L::kTileB, vb = kb + L::kTileB;
-    f32x16 x[RW][2];
+  // Per-lane places of the operands inside a tile; the rest is a constant.
+  // K: row 32 tb + c, chunk 2 ks + h.  V: token 16 st + 8 part + 4 h + l % 16 / 4,
+  // chunk 4 db + 2 (l / 16 % 2) + l % 4 / 2, half a chunk l % 2.
+  uint32_t ka[KS], va[DB];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) ka[ks] = lds + c * L::kRowB + (((2 * ks + hf) ^ (c & (L::CH - 1))) << 4);
+#pragma unroll
+  for (int db = 0; db < DB; ++db) {
+    const int r = 4 * hf + ((lane & 15) >> 2), chunk = 4 * db + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+    va[db] = lds + 3 * L::kTileB + r * L::kRowB + ((chunk ^ (2 * r & (L::CH - 1))) << 4) + 8 * (lane & 1);
+  }
+
+  // scores of a tile (raw products)
+  auto score = [&](int tile, f32x16 (&x)[RW][2]) {
+    const uint32_t off = (tile % 3) * L::kTileB;
 #pragma unroll
     for (int tb = 0; tb < 2; ++tb) {
 #pragma unroll
       for (int w = 0; w < RW; ++w) x[w][tb] = zero16();
-      const int r = 32 * tb + c;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        const u32x4 kf = lds_read16(kb + r * L::kRowB + (((2 * ks + hf) ^ (r & (L::CH - 1))) << 4));
+        const u32x4 kf = lds_read16(ka[ks] + off, tb * 32 * L::kRowB);
 #pragma unroll
         for (int w = 0; w < RW; ++w) x[w][tb] = mfma32<F16>(kf, qf[w][ks], x[w][tb]);
       }
     }
+  };
+  // hides what a row does not see
+  auto mask = [&](int tile, f32x16 (&x)[RW][2]) {
     const int u0 = tile * L::kTok, u1 = u0 + L::kTok - 1, ta = rg.token(u0), te = rg.token(u1);
-    const bool full = u1 < rg.cnt && ((ta >= full_lo && te < full_hi) || te < full_ns);
-    if (!full) {
-      hidden = true;
+    if (u1 < rg.cnt && ((ta >= full_lo && te < full_hi) || te < full_ns)) return;
+    hidden = true;
 #pragma unroll
-      for (int tb = 0; tb < 2; ++tb)
+    for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int u = u0 + 32 * tb + 8 * (r / 4) + 4 * hf + r % 4, t = rg.token(min(u, rg.cnt - 1));
-          const int pt = poss ? poss[t] : base + t;
+      for (int r = 0; r < 16; ++r) {
+        const int u = u0 + 32 * tb + 8 * (r / 4) + 4 * hf + r % 4, t = rg.token(min(u, rg.cnt - 1));
+        const int pt = poss ? poss[t] : base + t;
 #pragma unroll
-          for (int w = 0; w < RW; ++w)
-            x[w][tb][r] = u < rg.cnt && sees(pt, qp[w], a.window, a.n_sink) ? x[w][tb][r] : -INFINITY;
-        }
-    }
-    u32x4 ph[RW][4];
+        for (int w = 0; w < RW; ++w)
+          x[w][tb][r] = u < rg.cnt && sees(pt, qp[w], a.window, a.n_sink) ? x[w][tb][r] : -INFINITY;
+      }
+    // (vmcnt 0) the positions have arrived on every path: the compiler would
+    // wait behind the branch otherwise, and drain the tiles under way each time
+    __builtin_amdgcn_s_waitcnt(0x0F70);
+  };
+  auto largest = [&](const f32x16 (&x)[RW][2], float (&mx)[RW]) {
 #pragma unroll
     for (int w = 0; w < RW; ++w) {
-      float mx = -INFINITY;
+      mx[w] = -INFINITY;
 #pragma unroll
       for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, x[w][tb][r]);
-      mx = max32(mx) * a.sl2;
-      if (__ballot(mx > m[w] + kLag || (m[w] == -INFINITY && mx > m[w])) != 0ull) {
-        const float nm = mx > m[w] ? mx : m[w];
+        for (int r = 0; r < 16; r += 2) mx[w] = max3(mx[w], x[w][tb][r], x[w][tb][r + 1]);
+    }
+  };
+
+  // One step: the weights of tile t from its scores x (largest one of a lane
+  // mx), beside the scores of tile t + 1 (into y); then tile t's values beside
+  // the largest of y.  A wave issues in order, so the vector work is written
+  // between the products, and operands are read from LDS kAhead products early;
+  // the fences keep the compiler from gathering either.
+  auto step = [&](int t, f32x16 (&x)[RW][2], float (&mx)[RW], f32x16 (&y)[RW][2], float (&my)[RW]) {
+    float ref[RW];
+#pragma unroll
+    for (int w = 0; w < RW; ++w) {
+      const float top = max32(mx[w]) * a.sl2;
+      if (__ballot(top > m[w] + kLag || (m[w] == -INFINITY && top > m[w])) != 0ull) {
+        const float nm = top > m[w] ? top : m[w];
         const float al = nm == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[w] - nm);
         l[w] *= al;
 #pragma unroll
         for (int db = 0; db < DB; ++db) o[w][db] *= al;
         m[w] = nm;
       }
-      const float ref = m[w] == -INFINITY ? 0.f : m[w];
-      float sum = 0.f;
-#pragma unroll
-      for (int tb = 0; tb < 2; ++tb)
-#pragma unroll
-        for (int r = 0; r < 16; r += 2) {
-          const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[w][tb][r], a.sl2, -ref));
-          const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[w][tb][r + 1], a.sl2, -ref));
-          sum += p0 + p1;
-          ph[w][2 * tb + r / 8][(r % 8) / 2] = pack2<F16>(p0, p1);
-        }
-      l[w] += sum;
+      ref[w] = m[w] == -INFINITY ? 0.f : m[w];
     }
+    u32x4 ph[RW][4];
+    {
+      // past the last tile: what an older tile left, used by nobody
+      const uint32_t off = ((t + 1) % 3) * L::kTileB;
+      u32x4 kf[kAhead];
+      auto read = [&](int i) { return lds_read16(ka[i / 2] + off, (i % 2) * 32 * L::kRowB); };
 #pragma unroll
-    for (int st = 0; st < 4; ++st)            // 16 tokens
+      for (int i = 0; i < kAhead; ++i) kf[i] = read(i);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int db = 0; db < DB; ++db) {
-        u32x4 vf;
+      for (int i = 0; i < 2 * KS; ++i) {
 #pragma unroll
-        for (int part = 0; part < 2; ++part) {
-          const int r = 16 * st + 8 * part + 4 * hf + ((lane & 15) >> 2);
-          const int chunk = 4 * db + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-          const s16x4 t = lds_read_tr(vb + r * L::kRowB + ((chunk ^ (2 * r & (L::CH - 1))) << 4) + 8 * (lane & 1));
-          const uint2 x2 = __builtin_bit_cast(uint2, t);
-          vf[2 * part] = x2.x;
-          vf[2 * part + 1] = x2.y;
-        }
+        for (int w = 0; w < RW; ++w) y[w][i % 2] = mfma32<F16>(kf[i % kAhead], qf[w][i / 2], i < 2 ? zero16() : y[w][i % 2]);
+        if (i + kAhead < 2 * KS) kf[i % kAhead] = read(i + kAhead);
+        // the tile's 16 pairs of scores, over the 2 KS products
 #pragma unroll
-        for (int w = 0; w < RW; ++w) o[w][db] = mfma32<F16>(vf, ph[w][st], o[w][db]);
+        for (int w = 0; w < RW; ++w)
+#pragma unroll
+          for (int e = i * 16 / (2 * KS); e < (i + 1) * 16 / (2 * KS); ++e) {
+            const int tb = e / 8, r = 2 * (e % 8);
+            const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[w][tb][r], a.sl2, -ref[w]));
+            const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[w][tb][r + 1], a.sl2, -ref[w]));
+            l[w] += p0 + p1;
+            ph[w][e / 4][e % 4] = pack2<F16>(p0, p1);
+          }
+        __builtin_amdgcn_sched_barrier(0);
       }
+#pragma unroll
+      for (int w = 0; w < RW; ++w) {
+        // keeps the weights here, beside the products
+#pragma unroll
+        for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(ph[w][i]));
+        asm volatile("" : "+v"(l[w]));
+      }
+    }
+    if (t + 1 < tile1) mask(t + 1, y);
+    {
+      const uint32_t off = (t % 3) * L::kTileB;
+      u32x4 vf[kAhead];
+      auto read = [&](int i) {                   // 16 tokens i / DB, widths 32 (i % DB) ..
+        const uint2 p = __builtin_bit_cast(uint2, lds_read_tr(va[i % DB] + off, 16 * (i / DB) * L::kRowB));
+        const uint2 q = __builtin_bit_cast(uint2, lds_read_tr(va[i % DB] + off, (16 * (i / DB) + 8) * L::kRowB));
+        return u32x4{p.x, p.y, q.x, q.y};
+      };
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) vf[i] = read(i);
+#pragma unroll
+      for (int w = 0; w < RW; ++w) my[w] = -INFINITY;
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < 4 * DB; ++i) {
+#pragma unroll
+        for (int w = 0; w < RW; ++w) o[w][i % DB] = mfma32<F16>(vf[i % kAhead], ph[w][i / DB], o[w][i % DB]);
+        if (i + kAhead < 4 * DB) vf[i % kAhead] = read(i + kAhead);
+#pragma unroll
+        for (int w = 0; w < RW; ++w)
+#pragma unroll
+          for (int e = i * 16 / (4 * DB); e < (i + 1) * 16 / (4 * DB); ++e)
+            my[w] = max3(my[w], y[w][e / 8][2 * (e % 8)], y[w][e / 8][2 * (e % 8) + 1]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
   };
 
+  // A load step j brings V of tile j and K of tile j + 1; two steps are under way.
   constexpr int KV = 2 * L::LOADS, T = TAB ? 1 : 0;
   if (tile0 < tile1) {
 #pragma unroll
@@ -279,39 +356,49 @@ __global__ __launch_bounds__(64 * NW) void attend_wide_kernel(AttendArgs a, Spli
       asm volatile("" : "+v"(qp[w]));
     }
     wait_loads<0>();
-    load_tables(tile0);
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+      if (tile0 + i < tile1) load_tables(tile0 + i);
+    wait_loads<0>();
+    load_k(tile0);
+    if (tile0 + 1 < tile1) load_k(tile0 + 1);
+    load_v(tile0);
+    if (tile0 + 3 < tile1) load_tables(tile0 + 3);
     if (tile0 + 1 < tile1) {
-      load_tables(tile0 + 1);
-      wait_loads<T>();
-    } else {
-      wait_loads<0>();
+      if (tile0 + 2 < tile1) load_k(tile0 + 2);
+      load_v(tile0 + 1);
     }
-    load_tile(tile0);
-    if (tile0 + 1 < tile1) {
-      if (tile0 + 2 < tile1) {
-        load_tables(tile0 + 2);
-        wait_loads<KV + T>();
-      } else {
-        wait_loads<KV>();
-      }
-      load_tile(tile0 + 1);
-    }
-    for (int t = tile0; t < tile1; ++t) {
-      // under way, oldest first: tile(t), tables(t + 2), tile(t + 1)
-      if (t + 2 < tile1) wait_loads<T + KV>();
-      else if (t + 1 < tile1) wait_loads<KV>();
+    f32x16 xa[RW][2], xb[RW][2];
+    float ma[RW], mb[RW];
+    // under way, oldest first: step t, tables(t + 3), step t + 1
+    auto turn = [&](int t, bool first, f32x16 (&x)[RW][2], float (&mx)[RW], f32x16 (&y)[RW][2], float (&my)[RW]) {
+      if (t + 3 < tile1) wait_loads<T + KV>();
+      else if (t + 2 < tile1) wait_loads<KV>();
+      else if (t + 1 < tile1) wait_loads<L::LOADS>();
       else wait_loads<0>();
-      tile_barrier();             // tile t is there, and no wave reads tile t - 1 any more
+      tile_barrier();             // step t is there, and no wave reads step t - 1 any more
+      if (first && wave_on) {
+        score(t, x);
+        mask(t, x);
+        largest(x, mx);
+      }
+      if (first) tile_barrier();  // K of the first tile is read beside the others' next
       if (t + 2 < tile1) {
-        if (t + 3 < tile1) {
-          load_tables(t + 3);
+        if (t + 4 < tile1) {
+          load_tables(t + 4);
           wait_loads<KV + T>();
-        } else {
+        } else if (t + 3 < tile1) {
           wait_loads<KV>();
         }
-        load_tile(t + 2);
+        if (t + 3 < tile1) load_k(t + 3);
+        load_v(t + 2);
       }
-      if (wave_on) compute(t);
+      if (wave_on) step(t, x, mx, y, my);
+    };
+    turn(tile0, true, xa, ma, xb, mb);
+    for (int t = tile0 + 1; t < tile1; t += 2) {
+      turn(t, false, xb, mb, xa, ma);
+      if (t + 1 < tile1) turn(t + 1, false, xa, ma, xb, mb);
     }
   }
   wait_loads<0>();
