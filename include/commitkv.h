@@ -539,8 +539,8 @@ int ckv_select_and_compact(ckv_ctx* ctx, const ckv_cache_view* in,
  * n_tokens is on the DEVICE, so that a captured step serves growing caches;
  * max_tokens is the host's bound (larger and negative counts are clamped to
  * [0, max_tokens]; slot and pos rows hold max_tokens entries at least).
- * pos[s*pos_stride + t] is the token's absolute position, >= 0 and ascending
- * in t (with another order the calls stay in bounds, and which tokens a row
+ * pos[s*pos_stride + t] is the token's absolute position, >= 0 and strictly
+ * ascending in t (with another order the calls stay in bounds, and which tokens a row
  * sees is undefined).  NULL: token t is at position t, or, in
  * ckv_attend_shared, at position t behind the shared tokens. */
 typedef struct ckv_batch_view {

@@ -181,7 +181,7 @@ __global__ __launch_bounds__(Narrow<D>::NT) void attend_narrow_kernel(AttendArgs
       qmax = max(qmax, __shfl_xor(qmax, off, 64));
     }
   }
-  Range rg = seen_range(a.own, s, n, base, qmin, qmax, a.window, a.n_sink);
+  Range rg = seen_range(a.own, s, n, base, qmin, qmax, a.window, a.n_sink, !a.qpos && p_last == R - 1 && R <= n);
   rg.ns = __builtin_amdgcn_readfirstlane(rg.ns);
   rg.shift = __builtin_amdgcn_readfirstlane(rg.shift);
   rg.cnt = __builtin_amdgcn_readfirstlane(rg.cnt);
@@ -441,14 +441,13 @@ __global__ __launch_bounds__(Narrow<D>::NT) void attend_narrow_kernel(AttendArgs
   for (int i = tid; i < n_rows * TPR; i += NT) {
     const int row = i / TPR, w4 = (i % TPR) * 4;
     Joined all = {-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f}};
-    for (int j = 0; j < it.n_split; ++j) {
-      const int64_t at = (first + (int64_t)j * a.Hkv) * L::kRows + row;
-      const float pm = get_word(sp.ml + at * 2), pl = get_word(sp.ml + at * 2 + 1);
-      f32x4 po;
+    all.template add_all<16>(it.n_split, [&](int k, float& m, float& l, f32x4& o) {
+      const int64_t at = (first + (int64_t)k * a.Hkv) * L::kRows + row;
+      m = get_word(sp.ml + at * 2);
+      l = get_word(sp.ml + at * 2 + 1);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) po[e] = get_word(sp.o + at * D + w4 + e);
-      all.add(pm, pl, po);
-    }
+      for (int e = 0; e < 4; ++e) o[e] = get_word(sp.o + at * D + w4 + e);
+    });
     finish(row, w4, all);
   }
 }
@@ -473,9 +472,13 @@ AttendPlan plan_narrow(const AttendArgs& a, int64_t max_tokens, bool room) {
   p.rows = 16;
   const int64_t n_seq = std::min(a.own.n_seq, a.n_rows);
   const int64_t blocks = (int64_t)a.n_rows * a.group / 16 + n_seq;      // row blocks of a KV head, at most
-  const int64_t slots = 2 * 256;                                        // workgroups that run at once
-  p.target = (int)(2 * slots);
-  p.min_chunk = 256;
+  // 512 workgroups run at once.  Few row blocks are cut into one round of equal
+  // splits (two 128K sequences: 205 us, 246 with two rounds); with more, lengths
+  // differ from block to block and two rounds even them out (64 ragged
+  // sequences: 203 us, 212 with one).
+  const int64_t slots = 2 * 256;
+  p.target = (int)(blocks * a.Hkv < slots / 2 ? slots : 2 * slots);
+  p.min_chunk = 512;
   int64_t e = p.target / a.Hkv + blocks + 1;
   if (!room || max_tokens <= p.min_chunk || blocks * a.Hkv >= 4 * p.target) {
     p.min_chunk = INT_MAX;                                              // no splits

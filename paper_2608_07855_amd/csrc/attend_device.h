@@ -90,9 +90,20 @@ struct ItemShared {
   int found[4];
 };
 
-// Item e of a KV head: blocks of RB rows, about `target` items over all heads, at least min_chunk tokens each.
+__device__ __forceinline__ long long wave_scan(long long v) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const long long u = __shfl_up(v, off, 64);
+    if (lane >= off) v += u;
+  }
+  return v;
+}
+
+// Item e of a KV head: blocks of RB rows, about `target` items over all heads,
+// at least min_chunk tokens each.
 template <int NT, int RB>
-__device__ Item find_item(const AttendArgs& a, int64_t e, int target, int min_chunk, ItemShared& sh) {
+__device__ __forceinline__ Item find_item(const AttendArgs& a, int64_t e, int target, int min_chunk, ItemShared& sh) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n_seq = a.own.n_seq;
   auto load = [&](int s, int& nrb, int& est) {
     nrb = est = 0;
@@ -102,6 +113,31 @@ __device__ Item find_item(const AttendArgs& a, int64_t e, int target, int min_ch
       est = seen_estimate(a, seq_tokens(a.own, s), min(RB, R * a.group));
     }
   };
+  auto splits = [&](int est, int64_t chunk) { return est > 0 ? (int)((est + chunk - 1) / chunk) : 1; };
+  auto chunk_of = [&](long long work) {
+    return min_chunk == INT_MAX ? (int64_t)INT_MAX : max((int64_t)min_chunk, (work * a.Hkv + target - 1) / target);
+  };
+  Item it;
+  it.e = e;
+  if (n_seq <= 64) {
+    // every wave for itself, a sequence per lane
+    int nrb, est;
+    load(lane, nrb, est);
+    long long work = (long long)nrb * est;
+    if (min_chunk != INT_MAX)
+#pragma unroll
+      for (int off = 32; off; off >>= 1) work += __shfl_xor(work, off, 64);
+    const int n_split = splits(est, chunk_of(work));
+    const long long mine = (long long)nrb * n_split, at = e - (wave_scan(mine) - mine);
+    const unsigned long long who = __ballot(at >= 0 && at < mine);
+    const int s = who ? __ffsll(who) - 1 : 0;
+    it.s = who ? s : -1;
+    it.n_split = __builtin_amdgcn_readlane(n_split, s);
+    const int place = __builtin_amdgcn_readlane((int)at, s);
+    it.rb = place / it.n_split;
+    it.split = place % it.n_split;
+    return it;
+  }
   int nrb, est;
   load(tid, nrb, est);
   long long work = (long long)nrb * est;
@@ -110,20 +146,14 @@ __device__ Item find_item(const AttendArgs& a, int64_t e, int target, int min_ch
     load(s, b, t);
     work += (long long)b * t;
   }
-  work = block_sum<NT>(work, sh.wave) * a.Hkv;
-  const int64_t chunk = max((int64_t)min_chunk, (work + target - 1) / target);
+  const int64_t chunk = chunk_of(block_sum<NT>(work, sh.wave));
   if (tid == 0) sh.found[0] = -1;
   int64_t before = 0;
   for (int s0 = 0; s0 < n_seq; s0 += NT) {
     if (s0) load(s0 + tid, nrb, est);
-    const int n_split = est > 0 ? (int)((est + chunk - 1) / chunk) : 1;
+    const int n_split = splits(est, chunk);
     const long long mine = (long long)nrb * n_split;
-    long long v = mine;
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-      const long long u = __shfl_up(v, off, 64);
-      if (lane >= off) v += u;
-    }
+    long long v = wave_scan(mine);
     __syncthreads();
     if (lane == 63) sh.wave[wave] = v;
     __syncthreads();
@@ -144,33 +174,36 @@ __device__ Item find_item(const AttendArgs& a, int64_t e, int target, int min_ch
     if (before > e) break;
   }
   __syncthreads();
-  Item it;
   it.s = __builtin_amdgcn_readfirstlane(sh.found[0]);
   it.rb = __builtin_amdgcn_readfirstlane(sh.found[1]);
   it.split = __builtin_amdgcn_readfirstlane(sh.found[2]);
   it.n_split = __builtin_amdgcn_readfirstlane(sh.found[3]);
-  it.e = e;
   return it;
 }
 
-// First t of [0, n) with pos[t] > key (n if none), pos ascending: a wave
-// tries 64 places at once, so 131072 positions take three dependent loads.
-__device__ __forceinline__ int upper_bound(const int32_t* pos, int n, long long key) {
-  const int lane = threadIdx.x & 63;
-  int lo = 0, len = n;
-  while (len > 0) {
-    const int step = (len + 63) / 64;
-    const int t = lo + min(lane * step + step - 1, len - 1);     // last place of the lane's part
-    const bool le = pos[t] <= key && lane * step < len;
-    const int parts = __popcll(__ballot(le));                    // parts that lie at or below the key
-    const int skip = min(parts * step, len);
+// First t of [lo, lo + len) with pos[t] > key (its end if none), pos ascending:
+// a wave tries 64 places at once, so 4096 places take two dependent loads.
+struct Search {
+  const int32_t* pos;
+  int lo, len;
+  long long key;
+  int step, t;
+  __device__ __forceinline__ int probe() {      // the position to load
+    step = (len + 63) / 64;
+    t = lo + min((int)(threadIdx.x & 63) * step + step - 1, len - 1);   // last place of the lane's part
+    return len > 0 ? pos[t] : 0;
+  }
+  __device__ __forceinline__ void take(int value) {
+    if (len <= 0) return;
+    const bool le = value <= key && (int)(threadIdx.x & 63) * step < len;
+    const int skip = min(__popcll(__ballot(le)) * step, len);   // parts that lie at or below the key
     lo += skip;
     len = min(step - 1, len - skip);
   }
-  return lo;
-}
+};
 
-// The tokens that rows at positions qmin..qmax see between them, as one range
+// The tokens that rows at positions qmin..qmax see between them (tail_rows: of
+// these rows, one position is that of the sequence's last token), as one range
 // of indexes u < cnt: first tokens t = u < ns, then t = u + shift.
 struct Range {
   int ns, shift, cnt;
@@ -178,15 +211,27 @@ struct Range {
 };
 
 __device__ __forceinline__ Range seen_range(const SeqCaches& c, int sq, int n, int base, int qmin, int qmax, int window,
-                                            int n_sink) {
+                                            int n_sink, bool tail_rows = false) {
   int hi, lo = 0, ns = 0;
   if (c.pos) {
+    // Positions are distinct, so at most `window` tokens before the last seen
+    // one lie inside a window, and at most n_sink are first ones.  The three
+    // searches load together.
     const int32_t* p = c.pos + sq * c.pos_stride;
-    hi = upper_bound(p, n, qmax);
-    if (window) {
-      lo = upper_bound(p, n, (long long)qmin - window);
-      if (n_sink) ns = upper_bound(p, n, (long long)n_sink - 1);
+    const bool last = tail_rows && qmax == qmin;        // the row of the last token sees all of them
+    Search h = {p, 0, last ? 0 : n, (long long)qmax, 0, 0};
+    const int most = (int)min((long long)n, (long long)window + max((long long)qmax - qmin, 0ll));
+    Search w = {p, last ? n - most : 0, window ? (last ? most : n) : 0, (long long)qmin - window, 0, 0};
+    Search k = {p, 0, window ? min(n, n_sink) : 0, (long long)n_sink - 1, 0, 0};
+    while (max(max(h.len, w.len), k.len) > 0) {
+      const int a = h.probe(), b = w.probe(), d = k.probe();
+      h.take(a);
+      w.take(b);
+      k.take(d);
     }
+    hi = last ? n : h.lo;
+    lo = w.lo;
+    ns = k.lo;
   } else {
     auto in = [&](long long t) { return (int)min(max(t, 0ll), (long long)n); };
     hi = in((long long)qmax + 1 - base);
@@ -304,14 +349,31 @@ struct Joined {
     acc = acc * f0 + po * f1;
     m = nm;
   }
+  // n partial sums, in their order; the loads of N leave together
+  template <int N, class Load>
+  __device__ __forceinline__ void add_all(int n, Load load) {
+    for (int k0 = 0; k0 < n; k0 += N) {
+      float pm[N], pl[N];
+      f32x4 po[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) load(min(k0 + i, n - 1), pm[i], pl[i], po[i]);
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (k0 + i < n) add(pm[i], pl[i], po[i]);
+    }
+  }
 };
 
 __device__ __forceinline__ void add_prefix(const AttendArgs& a, const PrefixParts& pp, int D, int packed, int g, int w4, Joined& j) {
   const int64_t at0 = ((int64_t)(packed / pp.block_rows) * pp.n_split * a.Hkv + g) * pp.block_rows + packed % pp.block_rows;
-  for (int k = 0; k < pp.n_split; ++k) {
-    const int64_t at = at0 + (int64_t)k * a.Hkv * pp.block_rows;
-    j.add(pp.ml[at * 2], pp.ml[at * 2 + 1], *reinterpret_cast<const f32x4*>(pp.o + at * D + w4));
-  }
+  const int64_t stride = (int64_t)a.Hkv * pp.block_rows;
+  j.add_all<16>(pp.n_split, [&](int k, float& m, float& l, f32x4& o) {
+    const int64_t at = at0 + k * stride;
+    const float2 ml = *reinterpret_cast<const float2*>(pp.ml + at * 2);
+    m = ml.x;
+    l = ml.y;
+    o = *reinterpret_cast<const f32x4*>(pp.o + at * D + w4);
+  });
 }
 
 }  // namespace

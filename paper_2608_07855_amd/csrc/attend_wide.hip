@@ -485,10 +485,13 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, SplitSpa
   for (int i = blockIdx.y * 256 + threadIdx.x; i < n_rows * TPR; i += gridDim.y * 256) {
     const int row = i / TPR, w4 = (i % TPR) * 4;
     Joined j = {-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f}};
-    for (int k = 0; k < it.n_split; ++k) {
+    j.template add_all<16>(it.n_split, [&](int k, float& m, float& l, f32x4& o) {
       const int64_t at = ((int64_t)blockIdx.x + (int64_t)k * a.Hkv) * RB + row;
-      j.add(sp.ml[at * 2], sp.ml[at * 2 + 1], *reinterpret_cast<const f32x4*>(sp.o + at * D + w4));
-    }
+      const float2 ml = *reinterpret_cast<const float2*>(sp.ml + at * 2);
+      m = ml.x;
+      l = ml.y;
+      o = *reinterpret_cast<const f32x4*>(sp.o + at * D + w4);
+    });
     if (pp.n_split) add_prefix(a, pp, D, lead + row, g, w4, j);
     store_row<D, F16>(a, r0, it.rb * RB + row, g, w4, j.acc, j.m, j.l);
   }
@@ -519,7 +522,7 @@ PrefixPlan plan_prefix(const AttendArgs& a) {
   PrefixPlan p;
   p.rows = kRB;
   p.blocks = ((int64_t)a.n_rows * a.group + kRB - 1) / kRB;
-  const int64_t tiles = std::max<int64_t>(1, (a.pre.max_tokens + 63) / 64);
+  const int64_t tiles = std::max<int64_t>(1, (a.pre.max_tokens + 127) / 128);   // 128 tokens a split at least
   const int64_t wgs = p.blocks * a.Hkv;
   // as many splits as fill the device, then the count that leaves it least idle
   int64_t best = std::max<int64_t>(1, 256 / wgs);
