@@ -116,8 +116,8 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(AttendArgs a) {
 //
 // Bound: HBM (2 D 2 bytes a token and KV head against 16 x 32 x D x 4 FLOP a
 // tile on the matrix units), so what counts is loads under way: every wave has
-// its own two buffers of 32 tokens of K and V, filled by direct loads, without
-// any barrier between waves; slots and positions of the tile after the next
+// its own two buffers of 32 tokens of K and V (128 KB of LDS a compute unit),
+// filled by direct loads, without any barrier between waves; slots and positions of the tile after the next
 // travel the same way (one load of 32 words each).
 //
 // LDS: token r of a tile is row 4 (r % 8) + r / 8, so that a lane of load i
@@ -130,10 +130,9 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(AttendArgs a) {
 // rounded rest), both multiplied: the matrix units have time for it, and the
 // output keeps the precision of its own rounding.
 // ---------------------------------------------------------------------------
-template <int D>
+template <int D, int NW_>
 struct Narrow {
-  static constexpr int NW = 256 / D;                // waves: 64 KB of tiles a workgroup, two workgroups a compute unit
-  static constexpr int NT = 64 * NW;
+  static constexpr int NW = NW_, NT = 64 * NW;
   static constexpr int kRows = 16, kTok = 32;
   static constexpr int CH = D / 8;                  // 16-byte chunks of a row
   static constexpr int LANES = 64 / CH;             // tokens of one load
@@ -145,10 +144,10 @@ struct Narrow {
   __device__ static constexpr int row(int r) { return LANES * (r % LOADS) + r / LOADS; }
 };
 
-template <int D, bool F16, bool TAB>
-__global__ __launch_bounds__(Narrow<D>::NT) void attend_narrow_kernel(AttendArgs a, SplitSpace sp, int target, int min_chunk, PrefixParts pp) {
-  using L = Narrow<D>;
-  constexpr int NT = L::NT, NW = L::NW;
+template <int D, bool F16, bool TAB, int NW>
+__global__ __launch_bounds__(64 * NW) void attend_narrow_kernel(AttendArgs a, SplitSpace sp, int target, int min_chunk, PrefixParts pp) {
+  using L = Narrow<D, NW>;
+  constexpr int NT = L::NT;
   __shared__ __align__(16) char tiles[NW * L::kWaveB];
   __shared__ ItemShared ish;
   __shared__ float sm[NW][16], sl[NW][16];
@@ -472,13 +471,14 @@ AttendPlan plan_narrow(const AttendArgs& a, int64_t max_tokens, bool room) {
   p.rows = 16;
   const int64_t n_seq = std::min(a.own.n_seq, a.n_rows);
   const int64_t blocks = (int64_t)a.n_rows * a.group / 16 + n_seq;      // row blocks of a KV head, at most
-  // 512 workgroups run at once.  Few row blocks are cut into one round of equal
-  // splits (two 128K sequences: 205 us, 246 with two rounds); with more, lengths
-  // differ from block to block and two rounds even them out (64 ragged
-  // sequences: 203 us, 212 with one).
-  const int64_t slots = 2 * 256;
-  p.target = (int)(blocks * a.Hkv < slots / 2 ? slots : 2 * slots);
-  p.min_chunk = 512;
+  // Few row blocks: one round of equal splits on workgroups that have a compute
+  // unit's LDS to themselves (512 / D waves).  More: half as large workgroups,
+  // two a compute unit, so that one's prologue runs beside the other's loads;
+  // lengths differ from block to block, and two rounds even them out.
+  p.wide = blocks * a.Hkv <= 256;
+  p.target = p.wide ? 256 : 1024;
+  // Joining splits costs about 7 us; a split saves less below this length.
+  p.min_chunk = 2048;
   int64_t e = p.target / a.Hkv + blocks + 1;
   if (!room || max_tokens <= p.min_chunk || blocks * a.Hkv >= 4 * p.target) {
     p.min_chunk = INT_MAX;                                              // no splits
@@ -493,10 +493,12 @@ hipError_t launch_attend_narrow(const AttendArgs& a, const AttendPlan& p, const 
                                 hipStream_t s) {
   const dim3 grid((unsigned)p.items);
   const bool tab = a.own.slot || a.own.pos;
-#define CKV_NARROW(D, F16, TAB) attend_narrow_kernel<D, F16, TAB><<<grid, Narrow<D>::NT, 0, s>>>(a, sp, p.target, p.min_chunk, pp)
+#define CKV_NARROW(D, F16, TAB) \
+  if (p.wide) attend_narrow_kernel<D, F16, TAB, 512 / D><<<grid, 64 * 512 / D, 0, s>>>(a, sp, p.target, p.min_chunk, pp); \
+  else attend_narrow_kernel<D, F16, TAB, 256 / D><<<grid, 64 * 256 / D, 0, s>>>(a, sp, p.target, p.min_chunk, pp)
 #define CKV_NARROW2(D, F16) \
-  if (tab) CKV_NARROW(D, F16, true); \
-  else CKV_NARROW(D, F16, false)
+  if (tab) { CKV_NARROW(D, F16, true); } \
+  else { CKV_NARROW(D, F16, false); }
   if (a.D == 64) {
     if (a.f16) { CKV_NARROW2(64, true); } else { CKV_NARROW2(64, false); }
   } else {

@@ -504,6 +504,7 @@ constexpr int kRW = 1, kNW = 8, kRB = 32 * kRW * kNW;
 AttendPlan plan_wide(const AttendArgs& a, int64_t max_tokens, bool room) {
   AttendPlan p;
   p.rows = kRB;
+  p.wide = false;
   const int64_t n_seq = std::min(a.own.n_seq, a.n_rows);
   const int64_t blocks = (int64_t)a.n_rows * a.group / kRB + n_seq;     // row blocks of a KV head, at most
   p.target = 512;

@@ -426,6 +426,7 @@ struct AttendPlan {
   int64_t items;
   int rows, target, min_chunk;
   bool split;
+  bool wide;       // few-rows kernel: workgroups that take a compute unit each
 };
 AttendPlan plan_narrow(const AttendArgs& a, int64_t max_tokens, bool room);
 AttendPlan plan_wide(const AttendArgs& a, int64_t max_tokens, bool room);
