@@ -1824,50 +1824,51 @@ int attend(ckv_ctx* c, const ckv_batch_view* pre, const ckv_batch_view* kv, cons
   a.lse = lse;
   a.nonfinite = c->nf_dev;
   // Up to 32 rows a sequence and KV head take the few-rows kernel (blocks of
-  // 16, so K and V are read twice at most, the second time from L2).
+  // 16, so K and V are read twice at most, the second time from L2), the rows of
+  // all sequences together over the shared tokens before it.  More rows fill
+  // the matrix units by themselves: they read both parts in one pass.
   const bool few = (int64_t)q->max_rows * a.group <= 32;
-  auto plan = [&](bool room) { return few ? plan_narrow(a, kv->max_tokens, room) : plan_wide(a, kv->max_tokens, room); };
-  AttendPlan p = plan(true);
+  AttendPlan p = few ? plan_narrow(a, kv->max_tokens, true) : plan_wide(a, true);
   PrefixPlan pf = {0, 0, 0};
-  if (pre) pf = plan_prefix(a);
+  if (pre && few) pf = plan_prefix(a);
   auto floats = [&](int64_t items, int rows) { return round_up((size_t)items * rows * (a.D + 2) * sizeof(float), kAlign); };
   const int64_t pre_items = pf.blocks * pf.n_split * a.Hkv;
-  // the many-rows kernel leaves what shares a prefix to the join, split or not
-  auto own_bytes = [&] { return p.split || (pre && !few) ? floats(p.items, p.rows) : size_t(0); };
-  const size_t pre_bytes = pre ? floats(pre_items, pf.rows) : 0;
+  const size_t pre_bytes = floats(pre_items, pf.rows);
+  const size_t own_bytes = !p.split ? 0 : floats(p.items, p.rows) + (few ? 0 : p.items * sizeof(int4));
   bool room = true;
-  if (own_bytes() + pre_bytes > 0) {
+  if (own_bytes + pre_bytes > 0) {
     const size_t counts = few && p.split ? (size_t)p.items * sizeof(int) : 0;
-    if (int rc = ensure_attend_ws(c, counts, own_bytes() + pre_bytes, &room)) return rc;
-    if (!room) {
-      p = plan(false);
-      if (pre) {
-        CKV_LAUNCH(c, "attend", launch_attend_rows(a, c->stream));
-        return CKV_OK;
-      }
+    if (int rc = ensure_attend_ws(c, counts, own_bytes + pre_bytes, &room)) return rc;
+  }
+  if (!room) {
+    if (pre && few) {
+      CKV_LAUNCH(c, "attend", launch_attend_rows(a, c->stream));
+      return CKV_OK;
     }
+    p = few ? plan_narrow(a, kv->max_tokens, false) : plan_wide(a, false);
   }
   auto space = [&](size_t off, int64_t items, int rows) {
     SplitSpace sp;
     sp.arrive = reinterpret_cast<int*>(c->attend_ws.p);
     sp.o = reinterpret_cast<float*>(c->attend_ws.p + kAttendCounts + off);
     sp.ml = sp.o + items * rows * a.D;
+    sp.share = reinterpret_cast<int4*>(reinterpret_cast<char*>(sp.o) + floats(items, rows));
     return sp;
   };
-  const SplitSpace none = {nullptr, nullptr, nullptr};
-  const SplitSpace own = room && own_bytes() ? space(pre_bytes, p.items, p.rows) : none;
-  PrefixParts pp = {nullptr, nullptr, 0, 1};
-  if (pre) {
-    const SplitSpace sp = space(0, pre_items, pf.rows);
-    pp = {sp.o, sp.ml, pf.n_split, pf.rows};
-    CKV_LAUNCH(c, "attend_prefix", launch_attend_prefix(a, pf, sp, c->stream));
-  }
+  const SplitSpace none = {nullptr, nullptr, nullptr, nullptr};
+  const SplitSpace own = p.split ? space(pre_bytes, p.items, p.rows) : none;
   if (few) {
+    PrefixParts pp = {nullptr, nullptr, 0, 1};
+    if (pre) {
+      const SplitSpace sp = space(0, pre_items, pf.rows);
+      pp = {sp.o, sp.ml, pf.n_split, pf.rows};
+      CKV_LAUNCH(c, "attend_prefix", launch_attend_prefix(a, pf, sp, c->stream));
+    }
     CKV_LAUNCH(c, "attend", launch_attend_narrow(a, p, own, pp, c->stream));
     return CKV_OK;
   }
   CKV_LAUNCH(c, "attend", launch_attend_wide(a, p, own, c->stream));
-  if (p.split || pre) CKV_LAUNCH(c, "attend_join", launch_attend_join(a, p, own, pp, c->stream));
+  if (p.split) CKV_LAUNCH(c, "attend_join", launch_attend_join(a, p, own, c->stream));
   return CKV_OK;
 }
 

@@ -475,8 +475,8 @@ AttendPlan plan_narrow(const AttendArgs& a, int64_t max_tokens, bool room) {
   // unit's LDS to themselves (512 / D waves).  More: half as large workgroups,
   // two a compute unit, so that one's prologue runs beside the other's loads;
   // lengths differ from block to block, and two rounds even them out.
-  p.wide = blocks * a.Hkv <= 256;
-  p.target = p.wide ? 256 : 1024;
+  p.alone = blocks * a.Hkv <= 256;
+  p.target = p.alone ? 256 : 1024;
   // Joining splits costs about 7 us; a split saves less below this length.
   p.min_chunk = 2048;
   int64_t e = p.target / a.Hkv + blocks + 1;
@@ -494,7 +494,7 @@ hipError_t launch_attend_narrow(const AttendArgs& a, const AttendPlan& p, const 
   const dim3 grid((unsigned)p.items);
   const bool tab = a.own.slot || a.own.pos;
 #define CKV_NARROW(D, F16, TAB) \
-  if (p.wide) attend_narrow_kernel<D, F16, TAB, 512 / D><<<grid, 64 * 512 / D, 0, s>>>(a, sp, p.target, p.min_chunk, pp); \
+  if (p.alone) attend_narrow_kernel<D, F16, TAB, 512 / D><<<grid, 64 * 512 / D, 0, s>>>(a, sp, p.target, p.min_chunk, pp); \
   else attend_narrow_kernel<D, F16, TAB, 256 / D><<<grid, 64 * 256 / D, 0, s>>>(a, sp, p.target, p.min_chunk, pp)
 #define CKV_NARROW2(D, F16) \
   if (tab) { CKV_NARROW(D, F16, true); } \

@@ -207,6 +207,7 @@ struct Search {
 // of indexes u < cnt: first tokens t = u < ns, then t = u + shift.
 struct Range {
   int ns, shift, cnt;
+  int lo, hi, n_first;   // by token: from which on, and up to which, they may be seen; first tokens (before n_sink)
   __device__ __forceinline__ int token(int u) const { return u < ns ? u : u + shift; }
 };
 
@@ -243,6 +244,9 @@ __device__ __forceinline__ Range seen_range(const SeqCaches& c, int sq, int n, i
   lo = min(lo, hi);
   ns = min(ns, hi);
   Range r;
+  r.lo = lo;
+  r.hi = hi;
+  r.n_first = ns;
   if (lo <= ns) {
     r.ns = 0;
     r.shift = 0;
@@ -272,10 +276,10 @@ __device__ __forceinline__ uint32_t lds_at(const void* p) {
   return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
 }
 __device__ __forceinline__ void load_lds16(const void* g, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(g) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(g) : "memory");
 }
 __device__ __forceinline__ void load_lds4(const void* g, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(g) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(g) : "memory");
 }
 // until at most N of the wave's own global loads and stores are under way
 template <int N>

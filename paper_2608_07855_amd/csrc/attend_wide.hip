@@ -9,8 +9,10 @@ namespace ckv {
 namespace {
 
 // ---------------------------------------------------------------------------
-// Many rows: a workgroup takes NW x 32 RW query rows and streams tiles of 64
-// tokens through LDS; a wave keeps its rows' queries and outputs in registers.
+// A workgroup of 8 waves takes blocks of 256 query rows (a sequence's rows of
+// one KV head, position by position, the head's group of query heads
+// innermost) and streams tiles of 64 tokens through LDS; a wave keeps 32 rows'
+// queries and outputs in registers.
 //
 // S^T = K Q^T and O^T += V^T P^T on v_mfma_f32_32x32x16 (a row on lane column
 // c = l % 32, tokens 8 (r / 4) + 4 h + r % 4 with h = l / 32 and register r):
@@ -21,17 +23,28 @@ namespace {
 // The reference of the softmax weights follows a row's largest logit only
 // when that passes it by 2^8 (weights up to 256 keep their relative precision
 // in either type, sums are float32), so that the output is rarely rescaled.
+//
+// Bound: matrix and vector issue.  A step is 32 products (1024 cycles) and about
+// 140 vector instructions a wave; both waves of a SIMD pass the same barrier a
+// tile, so each interleaves the two for itself (see step()).
+//
+// Work is cut evenly: workgroup e of a KV head takes the same share of the
+// head's tokens-to-see as every other, wherever that begins and ends; a block
+// that falls into several shares leaves partial sums, which the join kernel
+// adds.  (Blocks as items of their own left the device idle in the last round:
+// 8 ragged chunks of 40 blocks 323 us.)
 // ---------------------------------------------------------------------------
 constexpr float kLag = 8.f;   // log2 units
 constexpr int kAhead = 4;     // operands read from LDS ahead of their products
+constexpr int kNW = 8, kNT = 64 * kNW, kRB = 32 * kNW, kTok = 64;
 
-template <int D, int RW, int NW>
+template <int D>
 struct Wide {
-  static constexpr int NT = 64 * NW, kRows = 32 * RW * NW, kTok = 64;
-  static constexpr int CH = D / 8, LANES = 64 / CH;
-  static constexpr int LOADS = kTok / LANES / NW;      // loads of a wave for a tile of K (or V)
+  static constexpr int CH = D / 8, LANES = 64 / CH;    // 16-byte chunks of a row, rows of a load
+  static constexpr int LOADS = kTok / LANES / kNW;     // loads of a wave for a tile of K (or V)
+  static constexpr int kOwn = LOADS * LANES;           // tokens of a tile that a wave loads
   static constexpr int kRowB = 2 * D, kTileB = kTok * kRowB;
-  static constexpr int kLds = 6 * kTileB + NW * 4 * 256;   // three tiles of K, three of V, four tables a wave
+  static constexpr int kLds = 6 * kTileB + kNW * 4 * 256;   // three tiles of K, three of V, four tables a wave
 };
 
 template <bool F16>
@@ -56,466 +69,686 @@ __device__ __forceinline__ uint32_t pack2(float x, float y) {
 
 __device__ __forceinline__ void tile_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// PRE: the rows of all sequences over the shared tokens, `n_split` splits;
-// partial sums only.  Otherwise a block of one sequence's rows.
-template <int D, bool F16, bool TAB, int RW, int NW, bool PRE>
-__global__ __launch_bounds__(64 * NW) void attend_wide_kernel(AttendArgs a, SplitSpace sp, int target, int min_chunk, int n_split) {
-  using L = Wide<D, RW, NW>;
-  constexpr int NT = L::NT, KS = D / 16, DB = D / 32;
-  __shared__ __align__(16) char tiles[L::kLds];
-  __shared__ ItemShared ish;
-  __shared__ int qlim[2][NW];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, hf = lane >> 5;
-  const SeqCaches& kv = PRE ? a.pre : a.own;
-  const int g = blockIdx.x % a.Hkv;
-  int s, rb, split, splits, r0, R;
-  if constexpr (PRE) {
-    s = 0;
-    split = (blockIdx.x / a.Hkv) % n_split;
-    rb = blockIdx.x / a.Hkv / n_split;
-    splits = n_split;
-    r0 = row_start(a, 0);
-    R = row_start(a, a.own.n_seq) - r0;
-    if ((int64_t)rb * L::kRows >= (int64_t)R * a.group) return;
-  } else {
-    const Item it = find_item<NT, L::kRows>(a, blockIdx.x / a.Hkv, target, min_chunk, ish);
-    if (it.s < 0) return;
-    s = it.s;
-    rb = it.rb;
-    split = it.split;
-    splits = it.n_split;
-    r0 = row_start(a, s);
-    R = row_start(a, s + 1) - r0;
-  }
-  const int n = seq_tokens(kv, s), pre_n = a.has_pre ? seq_tokens(a.pre, 0) : 0, base = PRE ? 0 : pre_n;
-  const int n_rows = min(L::kRows, R * a.group - rb * L::kRows);
+// the same in every lane
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ long long uniform(long long x) {
+  return (long long)((unsigned long long)(unsigned)uniform((int)x) | (unsigned long long)(unsigned)uniform((int)(x >> 32)) << 32);
+}
 
-  // the lane's rows: their positions and queries
-  int qp[RW];
-  u32x4 qf[RW][KS];
-  int qmin = INT_MAX, qmax = INT_MIN;
-  const bool wave_on = wave * 32 * RW < n_rows;
+// ---------------------------------------------------------------- shares
+
+// What the blocks of a sequence see, as far as the lengths tell, in tokens:
+// block rb sees shared + min(first + rb * step, cap).  It decides how blocks are
+// cut, not what they hold.
+struct BlockWork {
+  int shared, first, cap;
+  int step, n_blocks, n_below;   // n_below: blocks that see less than cap
+  // of the first k blocks
+  __device__ __forceinline__ long long sum(int k) const {
+    const int m = min(k, n_below);
+    return (long long)k * ((long long)shared + cap) + (long long)m * (first - cap) + (long long)m * (m - 1) / 2 * step;
+  }
+};
+
+__device__ __forceinline__ BlockWork block_work(const AttendArgs& a, int s, int shared) {
+  const int r0 = row_start(a, s), R = max(row_start(a, s + 1) - r0, 0), n = seq_tokens(a.own, s);
+  BlockWork w;
+  w.n_blocks = (int)(((int64_t)R * a.group + kRB - 1) / kRB);
+  w.step = max(kRB / a.group, 1);
+  w.shared = shared;
+  w.cap = max(a.window ? (int)min((long long)n, (long long)a.window + a.n_sink + w.step) : n, 1);
+  // rows at given positions may see all; else the last row of block 0 sees what lies before it
+  w.first = a.qpos ? w.cap : min(max(n - R + min(R, w.step), 1), w.cap);
+  w.n_below = (int)(((unsigned)(w.cap - w.first) + (unsigned)w.step - 1) / (unsigned)w.step);
+  return w;
+}
+// of a sequence that is the same in every lane
+__device__ __forceinline__ BlockWork uniform_work(const AttendArgs& a, int s, int shared) {
+  BlockWork w = block_work(a, s, shared);
+  w.first = uniform(w.first);
+  w.cap = uniform(w.cap);
+  w.n_below = uniform(w.n_below);
+  w.n_blocks = uniform(w.n_blocks);
+  return w;
+}
+
+// A share of a KV head's work: from place x of block rb of sequence s on.
+struct Share {
+  int s, rb;
+  long long x;      // inside the block
+  long long left;   // of the share
+  bool whole;       // blocks are not cut: workgroup e has block e (s, rb, x, left unset)
+};
+
+struct ShareShared {
+  ItemShared item;
+  int s;
+  long long at;
+};
+
+// Share e of W (fewer where that leaves less than four tiles each).  s < 0: none.
+// Cutting blocks costs about six tiles a share (partial sums written and
+// joined): where whole blocks end hardly later than that, they stay whole, and
+// blocks that run at the same time are neighbours (they share tiles in L2).
+template <int NT>
+__device__ __forceinline__ Share find_share(const AttendArgs& a, int e, int W, int shared, bool whole, ShareShared& sh) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n_seq = a.own.n_seq;
+  auto work = [&](int s, long long& blocks, long long& most) {
+    if (s >= n_seq) return 0ll;
+    const BlockWork w = block_work(a, s, shared);
+    blocks += w.n_blocks;
+    if (w.n_blocks) most = max(most, (long long)w.shared + w.cap);
+    return w.sum(w.n_blocks);
+  };
+  Share r = {-1, 0, 0, 0, whole};
+  if (whole) return r;
+  long long blocks = 0, most = 0, total = 0, mine = 0, upto = 0;
+  if (n_seq <= 64) {
+    mine = work(lane, blocks, most);
+    upto = wave_scan(mine);
+    total = __shfl(upto, 63, 64);
 #pragma unroll
-  for (int w = 0; w < RW; ++w) {
-    const int i = min((wave * RW + w) * 32 + c, n_rows - 1);
-    const int rr = rb * L::kRows + i, p = rr / a.group, h = g * a.group + rr % a.group;
-    if constexpr (PRE) {
-      const int row = r0 + p;
-      const int rs = max(row_seq(a, row), 0), f = row_start(a, rs);
-      qp[w] = row_position(a, rs, f, row_start(a, rs + 1) - f, row - f, seq_tokens(a.own, rs), pre_n);
-    } else {
-      qp[w] = row_position(a, s, r0, R, p, n, base);
+    for (int off = 32; off; off >>= 1) {
+      blocks += __shfl_xor(blocks, off, 64);
+      most = max(most, (long long)__shfl_xor(most, off, 64));
     }
-    const uint16_t* qr = a.q + (int64_t)(r0 + p) * a.q_row_stride + (int64_t)h * a.q_head_stride;
+  } else {
+    for (int s = tid; s < n_seq; s += NT) total += work(s, blocks, most);
+    total = block_sum<NT>(total, sh.item.wave);
+    blocks = block_sum<NT>(blocks, sh.item.wave);
+    __syncthreads();
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) qf[w][ks] = ldg_u4(qr + 16 * ks + 8 * hf);
-    qmin = min(qmin, qp[w]);
-    qmax = max(qmax, qp[w]);
+    for (int off = 32; off; off >>= 1) most = max(most, (long long)__shfl_xor(most, off, 64));
+    if (lane == 0) sh.item.wave[wave] = most;
+    __syncthreads();
+    for (int w = 0; w < NT / 64; ++w) most = max(most, sh.item.wave[w]);
   }
-#pragma unroll
-  for (int off = 16; off; off >>= 1) {
-    qmin = min(qmin, __shfl_xor(qmin, off, 64));
-    qmax = max(qmax, __shfl_xor(qmax, off, 64));
+  r.whole = (blocks + W - 1) / W * most <= total / W + 6 * kTok;
+  r.whole = uniform(r.whole);
+  if (r.whole || total == 0) return r;
+  const long long n = max(min((long long)W, total / (4 * kTok)), 1ll);
+  if (e >= n) return r;
+  const long long lo = (long long)((double)total * e / n), hi = e + 1 < n ? (long long)((double)total * (e + 1) / n) : total;
+  if (n_seq <= 64) {
+    const unsigned long long who = __ballot(lo >= upto - mine && lo < upto);
+    if (!who) return r;
+    r.s = __ffsll(who) - 1;
+    r.x = lo - __shfl(upto - mine, r.s, 64);
+  } else {
+    if (tid == 0) sh.s = -1;
+    long long before = 0;
+    for (int s0 = 0; s0 < n_seq; s0 += NT) {
+      mine = work(s0 + tid, blocks, most);
+      long long v = wave_scan(mine);
+      __syncthreads();
+      if (lane == 63) sh.item.wave[wave] = v;
+      __syncthreads();
+      long long all = 0;
+      for (int w = 0; w < NT / 64; ++w) {
+        if (w < wave) v += sh.item.wave[w];
+        all += sh.item.wave[w];
+      }
+      const long long at = lo - before - (v - mine);
+      if (at >= 0 && at < mine) {
+        sh.s = s0 + tid;
+        sh.at = at;
+      }
+      before += all;
+      if (before > lo) break;
+    }
+    __syncthreads();
+    if (sh.s < 0) return r;
+    r.s = sh.s;
+    r.x = sh.at;
   }
-  if (lane == 0) {
-    qlim[0][wave] = qmin;
-    qlim[1][wave] = qmax;
+  r.s = uniform(r.s);
+  r.x = uniform(r.x);
+  r.left = uniform(hi - lo);
+  // the block
+  const BlockWork w = uniform_work(a, r.s, shared);
+  int k0 = 0, k1 = w.n_blocks;
+  while (k1 - k0 > 1) {
+    const int k = (k0 + k1) >> 1;
+    if (w.sum(k) <= r.x) k0 = k;
+    else k1 = k;
   }
-  __syncthreads();
-  int bmin = qmin, bmax = qmax;
-#pragma unroll
-  for (int w = 0; w < NW; ++w) {
-    bmin = min(bmin, qlim[0][w]);
-    bmax = max(bmax, qlim[1][w]);
-  }
-  Range rg = seen_range(kv, s, n, base, bmin, bmax, a.window, a.n_sink);
-  rg.ns = __builtin_amdgcn_readfirstlane(rg.ns);
-  rg.shift = __builtin_amdgcn_readfirstlane(rg.shift);
-  rg.cnt = __builtin_amdgcn_readfirstlane(rg.cnt);
-  // tokens that every row of the wave sees: [full_lo, full_hi) and [0, full_ns)
-  int full_lo, full_hi, full_ns;
-  {
-    const Range all = seen_range(kv, s, n, base, qmax, qmin, a.window, a.n_sink);   // window of the last, end of the first
-    const bool joined = all.shift == 0;
-    full_hi = __builtin_amdgcn_readfirstlane(joined ? all.cnt : all.cnt + all.shift);
-    full_lo = __builtin_amdgcn_readfirstlane(joined ? 0 : all.ns + all.shift);
-    full_ns = __builtin_amdgcn_readfirstlane(all.ns);
-  }
-  const int n_tiles = (rg.cnt + L::kTok - 1) / L::kTok;
-  const int per_split = (n_tiles + splits - 1) / splits;
-  const int tile0 = min(split * per_split, n_tiles), tile1 = min(tile0 + per_split, n_tiles);
+  r.rb = uniform(k0);
+  r.x = uniform(r.x - w.sum(k0));
+  return r;
+}
 
+// first tile of place x of a part of `work` tokens that has n tiles
+__device__ __forceinline__ int tile_at(long long x, long long work, int n) {
+  if (x <= 0) return 0;
+  if (x >= work) return n;
+  return (int)min((long long)n, (x * n + work - 1) / work);
+}
+
+// The cache (or the shared tokens) that a block reads: its tokens and the
+// share's tiles of them.
+struct Part {
+  Range rg;
+  int n, base, sq, tile0, tile1;
+  int full_lo, full_hi;   // tokens that every row of the wave sees: [full_lo, full_hi), and first ones before full_hi
+  int row_lo, row_hi;     // tokens that the lane's row sees: [row_lo, row_hi), and first ones before row_hi
+};
+
+// PRE: the rows of all sequences over the shared tokens, in n_split splits, as
+// partial sums.  Otherwise a share of the blocks (W shares a KV head), in each
+// the shared tokens first; n_split 1: whole blocks only.
+template <int D, bool F16, bool TAB, bool PRE>
+__global__ __launch_bounds__(kNT) void attend_wide_kernel(AttendArgs a, SplitSpace sp, int W, int n_split) {
+  using L = Wide<D>;
+  constexpr int KS = D / 16, DB = D / 32;
+  __shared__ __align__(256) char tiles[L::kLds];
+  __shared__ ShareShared ssh;
+  __shared__ int qlim[2][kNW];
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), c = lane & 31, hf = lane >> 5;
+  const int g = blockIdx.x % a.Hkv, e = blockIdx.x / a.Hkv;
+  const int pre_n = a.has_pre ? uniform(seq_tokens(a.pre, 0)) : 0;
   const uint32_t lds = lds_at(tiles), tab = lds + 6 * L::kTileB + wave * 4 * 256;
   const int grp = lane / L::CH, ch = lane % L::CH;
-  constexpr int kOwn = L::LOADS * L::LANES;               // tokens of a tile that the wave loads
-  const int64_t head = g * kv.head_stride + (kv.slot ? 0 : s * kv.seq_stride);
-  const char* kh = reinterpret_cast<const char*>(kv.k + head);
-  const char* vh = reinterpret_cast<const char*>(kv.v + head);
-  const int32_t* slots = kv.slot ? kv.slot + s * kv.slot_stride : nullptr;
-  const int32_t* poss = kv.pos ? kv.pos + s * kv.pos_stride : nullptr;
-  const int64_t row_bytes = kv.tok_stride * 2;
-  auto token = [&](int tile, int r) { return rg.token(min(tile * L::kTok + r, rg.cnt - 1)); };
-  auto load_tables = [&](int tile) {
-    if constexpr (TAB) load_lds4(slots + token(tile, wave * kOwn + lane % kOwn), tab + (tile & 3) * 256);
-  };
-  // K of tile kt and V of tile vt travel together (V is needed one step later)
-  auto row_offset = [&](int tile, int i) -> int64_t {
-    int row;
-    if constexpr (TAB) {
-      const auto* w = (const __attribute__((address_space(3))) int*)(uintptr_t)(tab + (tile & 3) * 256);
-      row = (int)min((uint32_t)w[i * L::LANES + grp], (uint32_t)kv.pool_last);
-    } else {
-      row = token(tile, wave * kOwn + i * L::LANES + grp);
-    }
-    return row * row_bytes;
-  };
-  auto load_k = [&](int tile) {
-    const uint32_t kb = lds + (tile % 3) * L::kTileB;
-    int64_t at[L::LOADS];
-#pragma unroll
-    for (int i = 0; i < L::LOADS; ++i) at[i] = row_offset(tile, i);
-    wait_lds_reads();
-#pragma unroll
-    for (int i = 0; i < L::LOADS; ++i) {
-      const int r = wave * kOwn + i * L::LANES + grp;
-      load_lds16(kh + at[i] + ((ch ^ (r & (L::CH - 1))) << 4), kb + (wave * L::LOADS + i) * 1024);
-    }
-  };
-  auto load_v = [&](int tile) {
-    const uint32_t vb = lds + (3 + tile % 3) * L::kTileB;
-    int64_t at[L::LOADS];
-#pragma unroll
-    for (int i = 0; i < L::LOADS; ++i) at[i] = row_offset(tile, i);
-    wait_lds_reads();
-#pragma unroll
-    for (int i = 0; i < L::LOADS; ++i) {
-      const int r = wave * kOwn + i * L::LANES + grp;
-      load_lds16(vh + at[i] + ((ch ^ (2 * r & (L::CH - 1))) << 4), vb + (wave * L::LOADS + i) * 1024);
-    }
-  };
-
-  f32x16 o[RW][DB];
-  float m[RW], l[RW];
-#pragma unroll
-  for (int w = 0; w < RW; ++w) {
-    m[w] = -INFINITY;
-    l[w] = 0.f;
-#pragma unroll
-    for (int db = 0; db < DB; ++db) o[w][db] = zero16();
-  }
-  bool hidden = false;          // some tile held tokens that not all rows see
+  // where in its row the lane's chunk comes from (row r of a tile: chunk ch ^ r, for V ch ^ 2 r)
+  const uint32_t kc = (ch ^ ((wave * L::kOwn + grp) & (L::CH - 1))) << 4;
+  const uint32_t vc = (ch ^ (2 * (wave * L::kOwn + grp) & (L::CH - 1))) << 4;
 
   // Per-lane places of the operands inside a tile; the rest is a constant.
   // K: row 32 tb + c, chunk 2 ks + h.  V: token 16 st + 8 part + 4 h + l % 16 / 4,
-  // chunk 4 db + 2 (l / 16 % 2) + l % 4 / 2, half a chunk l % 2.
-  uint32_t ka[KS], va[DB];
-#pragma unroll
-  for (int ks = 0; ks < KS; ++ks) ka[ks] = lds + c * L::kRowB + (((2 * ks + hf) ^ (c & (L::CH - 1))) << 4);
-#pragma unroll
-  for (int db = 0; db < DB; ++db) {
-    const int r = 4 * hf + ((lane & 15) >> 2), chunk = 4 * db + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-    va[db] = lds + 3 * L::kTileB + r * L::kRowB + ((chunk ^ (2 * r & (L::CH - 1))) << 4) + 8 * (lane & 1);
+  // chunk 4 db + 2 (l / 16 % 2) + l % 4 / 2, half a chunk l % 2.  (The chunks of
+  // a row are exchanged by XOR with the token against bank conflicts.)
+  // Chunk 2 ks + h of token c lies at ((2 ks + h) ^ c) = (h ^ c) ^ 2 ks, so that
+  // one register an operand and a XOR give all of them.
+  const uint32_t ka = lds + c * L::kRowB + ((hf ^ (c & (L::CH - 1))) << 4);
+  uint32_t va;
+  {
+    const int r = 4 * hf + ((lane & 15) >> 2), chunk = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+    va = lds + 3 * L::kTileB + r * L::kRowB + ((chunk ^ (2 * r & (L::CH - 1))) << 4) + 8 * (lane & 1);
   }
 
-  // scores of a tile (raw products)
-  auto score = [&](int tile, f32x16 (&x)[RW][2]) {
-    const uint32_t off = (tile % 3) * L::kTileB;
-#pragma unroll
-    for (int tb = 0; tb < 2; ++tb) {
-#pragma unroll
-      for (int w = 0; w < RW; ++w) x[w][tb] = zero16();
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        const u32x4 kf = lds_read16(ka[ks] + off, tb * 32 * L::kRowB);
-#pragma unroll
-        for (int w = 0; w < RW; ++w) x[w][tb] = mfma32<F16>(kf, qf[w][ks], x[w][tb]);
-      }
+  Share me;
+  bool whole = false;
+  if constexpr (PRE) {
+    me = {0, e / n_split, 0, 1, false};
+  } else {
+    me = find_share<kNT>(a, e, W, pre_n, n_split != 0, ssh);
+    whole = me.whole;
+    if (sp.share && e < W && tid == 0 && (whole || me.s < 0)) sp.share[blockIdx.x] = make_int4(0, 0, 0, 0);
+    if (whole) {
+      const Item it = find_item<kNT, kRB>(a, e, 1, INT_MAX, ssh.item);
+      me = {it.s, it.rb, 0, 1, true};
     }
-  };
-  // hides what a row does not see
-  auto mask = [&](int tile, f32x16 (&x)[RW][2]) {
-    const int u0 = tile * L::kTok, u1 = u0 + L::kTok - 1, ta = rg.token(u0), te = rg.token(u1);
-    if (u1 < rg.cnt && ((ta >= full_lo && te < full_hi) || te < full_ns)) return;
-    hidden = true;
-#pragma unroll
-    for (int tb = 0; tb < 2; ++tb)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int u = u0 + 32 * tb + 8 * (r / 4) + 4 * hf + r % 4, t = rg.token(min(u, rg.cnt - 1));
-        const int pt = poss ? poss[t] : base + t;
-#pragma unroll
-        for (int w = 0; w < RW; ++w)
-          x[w][tb][r] = u < rg.cnt && sees(pt, qp[w], a.window, a.n_sink) ? x[w][tb][r] : -INFINITY;
+    if (me.s < 0) return;
+  }
+  int4 record = make_int4(0, 0, 0, 0);
+  for (bool opening = true; me.left > 0; opening = false) {
+    if (!opening) tile_barrier();          // the block before is done with LDS
+    // the share's part of this block
+    const int s = me.s, rb = me.rb;
+    const int r0 = uniform(row_start(a, PRE ? 0 : s)), R = uniform(row_start(a, PRE ? a.own.n_seq : s + 1)) - r0;
+    if (PRE && (int64_t)rb * kRB >= (int64_t)R * a.group) return;
+    const int n_rows = min(kRB, R * a.group - rb * kRB);
+    long long x0 = 0, x1 = 0, work = 0;
+    if constexpr (!PRE) {
+      const BlockWork w = uniform_work(a, s, pre_n);
+      work = w.sum(rb + 1) - w.sum(rb);
+      x0 = me.x;
+      x1 = whole ? work : min(work, x0 + me.left);
+      me.left -= x1 - x0;
+      me.x = 0;
+      if (++me.rb >= w.n_blocks && me.left > 0) {
+        me.rb = 0;
+        do ++me.s;
+        while (me.s < a.own.n_seq && uniform(row_start(a, me.s)) >= uniform(row_start(a, me.s + 1)));
+        if (me.s >= a.own.n_seq) me.left = 0;
       }
-    // (vmcnt 0) the positions have arrived on every path: the compiler would
-    // wait behind the branch otherwise, and drain the tiles under way each time
-    __builtin_amdgcn_s_waitcnt(0x0F70);
-  };
-  auto largest = [&](const f32x16 (&x)[RW][2], float (&mx)[RW]) {
-#pragma unroll
-    for (int w = 0; w < RW; ++w) {
-      mx[w] = -INFINITY;
-#pragma unroll
-      for (int tb = 0; tb < 2; ++tb)
-#pragma unroll
-        for (int r = 0; r < 16; r += 2) mx[w] = max3(mx[w], x[w][tb][r], x[w][tb][r + 1]);
+    } else {
+      me.left = 0;
     }
-  };
 
-  // One step: the weights of tile t from its scores x (largest one of a lane
-  // mx), beside the scores of tile t + 1 (into y); then tile t's values beside
-  // the largest of y.  A wave issues in order, so the vector work is written
-  // between the products, and operands are read from LDS kAhead products early;
-  // the fences keep the compiler from gathering either.
-  auto step = [&](int t, f32x16 (&x)[RW][2], float (&mx)[RW], f32x16 (&y)[RW][2], float (&my)[RW]) {
-    float ref[RW];
-#pragma unroll
-    for (int w = 0; w < RW; ++w) {
-      const float top = max32(mx[w]) * a.sl2;
-      if (__ballot(top > m[w] + kLag || (m[w] == -INFINITY && top > m[w])) != 0ull) {
-        const float nm = top > m[w] ? top : m[w];
-        const float al = nm == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[w] - nm);
-        l[w] *= al;
-#pragma unroll
-        for (int db = 0; db < DB; ++db) o[w][db] *= al;
-        m[w] = nm;
-      }
-      ref[w] = m[w] == -INFINITY ? 0.f : m[w];
+    // the lane's row: its position and query
+    const int i = min(wave * 32 + c, n_rows - 1);
+    const int rr = rb * kRB + i, p = rr / a.group, h = g * a.group + rr % a.group;
+    int qp;
+    if constexpr (PRE) {
+      const int row = r0 + p, rs = max(row_seq(a, row), 0), f = row_start(a, rs);
+      qp = row_position(a, rs, f, row_start(a, rs + 1) - f, row - f, seq_tokens(a.own, rs), pre_n);
+    } else {
+      qp = row_position(a, s, r0, R, p, seq_tokens(a.own, s), pre_n);
     }
-    u32x4 ph[RW][4];
-    {
-      // past the last tile: what an older tile left, used by nobody
-      const uint32_t off = ((t + 1) % 3) * L::kTileB;
-      u32x4 kf[kAhead];
-      auto read = [&](int i) { return lds_read16(ka[i / 2] + off, (i % 2) * 32 * L::kRowB); };
+    u32x4 qf[KS];
+    const uint16_t* qr = a.q + (int64_t)(r0 + p) * a.q_row_stride + (int64_t)h * a.q_head_stride;
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) kf[i] = read(i);
-      __builtin_amdgcn_sched_barrier(0);
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = ldg_u4(qr + 16 * ks + 8 * hf);
+    const bool wave_on = wave * 32 < n_rows;
+    int qmin = qp, qmax = qp;
 #pragma unroll
-      for (int i = 0; i < 2 * KS; ++i) {
+    for (int off = 16; off; off >>= 1) {
+      qmin = min(qmin, __shfl_xor(qmin, off, 64));
+      qmax = max(qmax, __shfl_xor(qmax, off, 64));
+    }
+    if (lane == 0) {
+      qlim[0][wave] = qmin;
+      qlim[1][wave] = qmax;
+    }
+    __syncthreads();
+    int bmin = qmin, bmax = qmax;
 #pragma unroll
-        for (int w = 0; w < RW; ++w) y[w][i % 2] = mfma32<F16>(kf[i % kAhead], qf[w][i / 2], i < 2 ? zero16() : y[w][i % 2]);
-        if (i + kAhead < 2 * KS) kf[i % kAhead] = read(i + kAhead);
-        // the tile's 16 pairs of scores, over the 2 KS products
+    for (int w = 0; w < kNW; ++w) {
+      bmin = min(bmin, qlim[0][w]);
+      bmax = max(bmax, qlim[1][w]);
+    }
+    qmin = uniform(qmin);
+    qmax = uniform(qmax);
+    bmin = uniform(bmin);
+    bmax = uniform(bmax);
+
+    f32x16 o[DB];
+    float m = -INFINITY, l = 0.f;
 #pragma unroll
-        for (int w = 0; w < RW; ++w)
-#pragma unroll
-          for (int e = i * 16 / (2 * KS); e < (i + 1) * 16 / (2 * KS); ++e) {
-            const int tb = e / 8, r = 2 * (e % 8);
-            const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[w][tb][r], a.sl2, -ref[w]));
-            const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[w][tb][r + 1], a.sl2, -ref[w]));
-            l[w] += p0 + p1;
-            ph[w][e / 4][e % 4] = pack2<F16>(p0, p1);
+    for (int db = 0; db < DB; ++db) o[db] = zero16();
+    bool hidden = false;          // some tile held tokens that not all rows see
+
+    auto caches = [&](int k) -> const SeqCaches& { return k ? a.own : a.pre; };
+    auto open = [&](int k) {
+      const SeqCaches& kv = caches(k);
+      Part t;
+      t.sq = k ? s : 0;
+      t.n = uniform(seq_tokens(kv, t.sq));
+      t.base = k ? pre_n : 0;
+      t.rg = seen_range(kv, t.sq, t.n, t.base, bmin, bmax, a.window, a.n_sink);
+      t.rg.ns = uniform(t.rg.ns);
+      t.rg.shift = uniform(t.rg.shift);
+      t.rg.cnt = uniform(t.rg.cnt);
+      t.rg.lo = uniform(t.rg.lo);
+      t.rg.hi = uniform(t.rg.hi);
+      t.rg.n_first = uniform(t.rg.n_first);
+      const Range all = seen_range(kv, t.sq, t.n, t.base, qmax, qmin, a.window, a.n_sink);   // window of the last, end of the first
+      t.full_hi = uniform(all.hi);
+      t.full_lo = uniform(all.lo);
+      if (kv.pos) {
+        // between the wave's first row and the block's last one (lane by lane)
+        const int32_t* pos = kv.pos + t.sq * kv.pos_stride;
+        auto find = [&](int lo, int hi, long long key) {      // first token with a position past key
+          while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (pos[mid] <= key) lo = mid + 1;
+            else hi = mid;
           }
-        __builtin_amdgcn_sched_barrier(0);
+          return lo;
+        };
+        t.row_hi = find(t.full_hi, t.rg.hi, qp);
+        t.row_lo = a.window ? find(t.rg.lo, t.rg.hi, (long long)qp - a.window) : 0;
+      } else {
+        auto in = [&](long long x) { return (int)min(max(x, 0ll), (long long)t.n); };
+        t.row_hi = in((long long)qp + 1 - t.base);
+        t.row_lo = a.window ? in((long long)qp - a.window + 1 - t.base) : 0;
       }
-#pragma unroll
-      for (int w = 0; w < RW; ++w) {
-        // keeps the weights here, beside the products
-#pragma unroll
-        for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(ph[w][i]));
-        asm volatile("" : "+v"(l[w]));
+      const int n_tiles = (t.rg.cnt + kTok - 1) / kTok;
+      if constexpr (PRE) {
+        const int split = e % n_split, per = (n_tiles + n_split - 1) / n_split;
+        t.tile0 = min(split * per, n_tiles);
+        t.tile1 = min(t.tile0 + per, n_tiles);
+      } else {
+        const long long from = k ? pre_n : 0, len = k ? work - pre_n : pre_n;
+        t.tile0 = uniform(tile_at(x0 - from, len, n_tiles));
+        t.tile1 = uniform(tile_at(x1 - from, len, n_tiles));
       }
-    }
-    if (t + 1 < tile1) mask(t + 1, y);
-    {
-      const uint32_t off = (t % 3) * L::kTileB;
-      u32x4 vf[kAhead];
-      auto read = [&](int i) {                   // 16 tokens i / DB, widths 32 (i % DB) ..
-        const uint2 p = __builtin_bit_cast(uint2, lds_read_tr(va[i % DB] + off, 16 * (i / DB) * L::kRowB));
-        const uint2 q = __builtin_bit_cast(uint2, lds_read_tr(va[i % DB] + off, (16 * (i / DB) + 8) * L::kRowB));
-        return u32x4{p.x, p.y, q.x, q.y};
-      };
-#pragma unroll
-      for (int i = 0; i < kAhead; ++i) vf[i] = read(i);
-#pragma unroll
-      for (int w = 0; w < RW; ++w) my[w] = -INFINITY;
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int i = 0; i < 4 * DB; ++i) {
-#pragma unroll
-        for (int w = 0; w < RW; ++w) o[w][i % DB] = mfma32<F16>(vf[i % kAhead], ph[w][i / DB], o[w][i % DB]);
-        if (i + kAhead < 4 * DB) vf[i % kAhead] = read(i + kAhead);
-#pragma unroll
-        for (int w = 0; w < RW; ++w)
-#pragma unroll
-          for (int e = i * 16 / (4 * DB); e < (i + 1) * 16 / (4 * DB); ++e)
-            my[w] = max3(my[w], y[w][e / 8][2 * (e % 8)], y[w][e / 8][2 * (e % 8) + 1]);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    }
-  };
-
-  // A load step j brings V of tile j and K of tile j + 1; two steps are under way.
-  constexpr int KV = 2 * L::LOADS, T = TAB ? 1 : 0;
-  if (tile0 < tile1) {
-#pragma unroll
-    for (int w = 0; w < RW; ++w) {
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qf[w][ks]));
-      asm volatile("" : "+v"(qp[w]));
-    }
-    wait_loads<0>();
-#pragma unroll
-    for (int i = 0; i < 3; ++i)
-      if (tile0 + i < tile1) load_tables(tile0 + i);
-    wait_loads<0>();
-    load_k(tile0);
-    if (tile0 + 1 < tile1) load_k(tile0 + 1);
-    load_v(tile0);
-    if (tile0 + 3 < tile1) load_tables(tile0 + 3);
-    if (tile0 + 1 < tile1) {
-      if (tile0 + 2 < tile1) load_k(tile0 + 2);
-      load_v(tile0 + 1);
-    }
-    f32x16 xa[RW][2], xb[RW][2];
-    float ma[RW], mb[RW];
-    // under way, oldest first: step t, tables(t + 3), step t + 1
-    auto turn = [&](int t, bool first, f32x16 (&x)[RW][2], float (&mx)[RW], f32x16 (&y)[RW][2], float (&my)[RW]) {
-      if (t + 3 < tile1) wait_loads<T + KV>();
-      else if (t + 2 < tile1) wait_loads<KV>();
-      else if (t + 1 < tile1) wait_loads<L::LOADS>();
-      else wait_loads<0>();
-      tile_barrier();             // step t is there, and no wave reads step t - 1 any more
-      if (first && wave_on) {
-        score(t, x);
-        mask(t, x);
-        largest(x, mx);
-      }
-      if (first) tile_barrier();  // K of the first tile is read beside the others' next
-      if (t + 2 < tile1) {
-        if (t + 4 < tile1) {
-          load_tables(t + 4);
-          wait_loads<KV + T>();
-        } else if (t + 3 < tile1) {
-          wait_loads<KV>();
-        }
-        if (t + 3 < tile1) load_k(t + 3);
-        load_v(t + 2);
-      }
-      if (wave_on) step(t, x, mx, y, my);
+      return t;
     };
-    turn(tile0, true, xa, ma, xb, mb);
-    for (int t = tile0 + 1; t < tile1; t += 2) {
-      turn(t, false, xb, mb, xa, ma);
-      if (t + 1 < tile1) turn(t + 1, false, xa, ma, xb, mb);
-    }
-  }
-  wait_loads<0>();
-  if (!wave_on) return;
 
+    for (int k = a.has_pre ? 0 : 1; k < (PRE ? 1 : 2); ++k) {
+      const SeqCaches& kv = caches(k);
+      const Part pt = open(k);
+      const Range rg = pt.rg;
+      const int tile0 = pt.tile0, tile1 = pt.tile1;
+      const int64_t head = g * kv.head_stride + (kv.slot ? 0 : pt.sq * kv.seq_stride);
+      const char* kh = reinterpret_cast<const char*>(kv.k + head);
+      const char* vh = reinterpret_cast<const char*>(kv.v + head);
+      const int32_t* slots = kv.slot ? kv.slot + pt.sq * kv.slot_stride : nullptr;
+      const int64_t row_bytes = kv.tok_stride * 2;
+      auto token = [&](int tile, int r) { return rg.token(min(tile * kTok + r, rg.cnt - 1)); };
+      // (where only the other part has a table, any word keeps the count of loads)
+      auto load_tables = [&](int tile) {
+        if constexpr (TAB)
+          load_lds4(slots ? slots + token(tile, wave * L::kOwn + lane % L::kOwn) : a.cu_rows, tab + (tile & 3) * 256);
+      };
+      auto row_offset = [&](int tile, int j) -> int64_t {
+        int row;
+        if (TAB && slots) {
+          const auto* w = (const __attribute__((address_space(3))) int*)(uintptr_t)(tab + (tile & 3) * 256);
+          row = (int)min((uint32_t)w[j * L::LANES + grp], (uint32_t)kv.pool_last);
+        } else {
+          row = token(tile, wave * L::kOwn + j * L::LANES + grp);
+        }
+        return row * row_bytes;
+      };
+      // K (at lane constant kc) or V of a tile; load j's rows are LANES j further
+      auto load_rows = [&](int tile, const char* from, uint32_t lane_c, uint32_t step_c, uint32_t to) {
+        int64_t at[L::LOADS];
 #pragma unroll
-  for (int w = 0; w < RW; ++w) {
-    l[w] = sum32(l[w]);
-    if (hidden) {
-      // as in the few-rows kernel: values that are not finite under a weight of 0
-      bool bad = !__builtin_isfinite(l[w]);
+        for (int j = 0; j < L::LOADS; ++j) at[j] = row_offset(tile, j);
+        wait_lds_reads();
+        // (opaque, or the compiler keeps a 64-bit sum for every load in registers)
+        asm volatile("" : "+v"(lane_c));
 #pragma unroll
-      for (int db = 0; db < DB; ++db)
+        for (int j = 0; j < L::LOADS; ++j)
+          load_lds16(from + (at[j] + (lane_c ^ (j * step_c))), to + (wave * L::LOADS + j) * 1024);
+      };
+      auto load_k = [&](int tile) { load_rows(tile, kh, kc, (L::LANES & (L::CH - 1)) << 4, lds + (tile % 3) * L::kTileB); };
+      auto load_v = [&](int tile) {
+        load_rows(tile, vh, vc, (2 * L::LANES & (L::CH - 1)) << 4, lds + (3 + tile % 3) * L::kTileB);
+      };
+
+      // scores of a tile (raw products)
+      auto score = [&](int tile, f32x16 (&x)[2]) {
+        const uint32_t off = (tile % 3) * L::kTileB;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) bad |= !__builtin_isfinite(o[w][db][r]);
-      if (__ballot(bad) != 0ull) {
+        for (int tb = 0; tb < 2; ++tb) {
+          x[tb] = zero16();
 #pragma unroll
-        for (int db = 0; db < DB; ++db) o[w][db] = zero16();
-        m[w] = -INFINITY;
-        l[w] = 0.f;
-        for (int u = tile0 * L::kTok; u < min(tile1 * L::kTok, rg.cnt); ++u) {
-          const int t = rg.token(u);
-          const int64_t at = (slots ? (int)min((uint32_t)slots[t], (uint32_t)kv.pool_last) : t) * row_bytes;
-          float x = 0.f;
+          for (int ks = 0; ks < KS; ++ks) x[tb] = mfma32<F16>(lds_read16((ka + off) ^ (32 * ks), tb * 32 * L::kRowB), qf[ks], x[tb]);
+        }
+      };
+      // hides what a row does not see
+      auto mask = [&](int tile, f32x16 (&x)[2]) {
+        const int u0 = tile * kTok, u1 = u0 + kTok - 1, ta = rg.token(u0), te = rg.token(u1);
+        if (te < pt.full_hi && (ta >= pt.full_lo || te < rg.n_first)) return;
+        hidden = true;
+        if (ta >= rg.n_first && u0 >= rg.ns) {
+          const uint32_t len = max(pt.row_hi - pt.row_lo, 0), d = ta + 4 * hf - pt.row_lo;
 #pragma unroll
-          for (int ks = 0; ks < KS; ++ks) {
-            const u32x4 kk = ldg_u4(kh + at + (16 * ks + 8 * hf) * 2);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x = fmaf(elem<F16>(chunk_elem(kk, e)), elem<F16>(chunk_elem(qf[w][ks], e)), x);
-          }
-          x = sum32(x) * a.sl2;
-          if (!sees(poss ? poss[t] : base + t, qp[w], a.window, a.n_sink)) continue;
-          const float nm = fmaxf(m[w], x), ref = nm == -INFINITY ? 0.f : nm;
-          const float al = __builtin_amdgcn_exp2f(m[w] - ref), p = __builtin_amdgcn_exp2f(x - ref);
-          m[w] = nm;
-          l[w] = l[w] * al + p;
-#pragma unroll
-          for (int db = 0; db < DB; ++db)
+          for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
             for (int r = 0; r < 16; ++r)
-              o[w][db][r] = fmaf(p, elem<F16>(reinterpret_cast<const uint16_t*>(vh + at)[32 * db + 8 * (r / 4) + 4 * hf + r % 4]),
-                                 o[w][db][r] * al);
+              x[tb][r] = d + (uint32_t)(32 * tb + 8 * (r / 4) + r % 4) < len ? x[tb][r] : -INFINITY;
+          return;
+        }
+#pragma unroll
+        for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int t = rg.token(u0 + 32 * tb + 8 * (r / 4) + 4 * hf + r % 4);
+            x[tb][r] = t < pt.row_hi && (t >= pt.row_lo || t < rg.n_first) ? x[tb][r] : -INFINITY;
+          }
+      };
+
+      // One step: the weights of tile t from its scores x (largest one of a lane
+      // mx), beside the scores of tile t + 1 (into y); then tile t's values beside
+      // the largest of y.  A wave issues in order, so the vector work is written
+      // between the products, and operands are read from LDS kAhead products
+      // early; the fences keep the compiler from gathering either.
+      auto step = [&](int t, f32x16 (&x)[2], float& mx, f32x16 (&y)[2], float& my) {
+        const float top = max32(mx) * a.sl2;
+        if (__ballot(top > m + kLag || (m == -INFINITY && top > m)) != 0ull) {
+          const float nm = top > m ? top : m;
+          const float al = nm == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - nm);
+          l *= al;
+#pragma unroll
+          for (int db = 0; db < DB; ++db) o[db] *= al;
+          m = nm;
+        }
+        const float ref = m == -INFINITY ? 0.f : m;
+        u32x4 ph[4];
+        {
+          // past the last tile: what an older tile left, used by nobody
+          const uint32_t off = ((t + 1) % 3) * L::kTileB;
+          u32x4 kf[kAhead];
+          auto read = [&](int j) { return lds_read16((ka + off) ^ (32 * (j / 2)), (j % 2) * 32 * L::kRowB); };
+#pragma unroll
+          for (int j = 0; j < kAhead; ++j) kf[j] = read(j);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int j = 0; j < 2 * KS; ++j) {
+            y[j % 2] = mfma32<F16>(kf[j % kAhead], qf[j / 2], j < 2 ? zero16() : y[j % 2]);
+            if (j + kAhead < 2 * KS) kf[j % kAhead] = read(j + kAhead);
+            // the tile's 16 pairs of scores, over the 2 KS products
+#pragma unroll
+            for (int q = j * 16 / (2 * KS); q < (j + 1) * 16 / (2 * KS); ++q) {
+              const int tb = q / 8, r = 2 * (q % 8);
+              const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[tb][r], a.sl2, -ref));
+              const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[tb][r + 1], a.sl2, -ref));
+              l += p0 + p1;
+              ph[q / 4][q % 4] = pack2<F16>(p0, p1);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+          }
+          // keeps the weights here, beside the products
+#pragma unroll
+          for (int j = 0; j < 4; ++j) asm volatile("" : "+v"(ph[j]));
+          asm volatile("" : "+v"(l));
+        }
+        if (t + 1 < tile1) mask(t + 1, y);
+        {
+          const uint32_t off = (t % 3) * L::kTileB;
+          u32x4 vf[kAhead];
+          auto read = [&](int j) {                   // tokens 16 (j / DB) .., widths 32 (j % DB) ..
+            const uint2 u = __builtin_bit_cast(uint2, lds_read_tr((va + off) ^ (64 * (j % DB)), 16 * (j / DB) * L::kRowB));
+            const uint2 v = __builtin_bit_cast(uint2, lds_read_tr((va + off) ^ (64 * (j % DB)), (16 * (j / DB) + 8) * L::kRowB));
+            return u32x4{u.x, u.y, v.x, v.y};
+          };
+#pragma unroll
+          for (int j = 0; j < kAhead; ++j) vf[j] = read(j);
+          my = -INFINITY;
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int j = 0; j < 4 * DB; ++j) {
+            o[j % DB] = mfma32<F16>(vf[j % kAhead], ph[j / DB], o[j % DB]);
+            if (j + kAhead < 4 * DB) vf[j % kAhead] = read(j + kAhead);
+#pragma unroll
+            for (int q = j * 16 / (4 * DB); q < (j + 1) * 16 / (4 * DB); ++q)
+              my = max3(my, y[q / 8][2 * (q % 8)], y[q / 8][2 * (q % 8) + 1]);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
+      };
+
+      // A load step j brings V of tile j and K of tile j + 1; two are under way.
+      constexpr int KV = 2 * L::LOADS, T = TAB ? 1 : 0;
+      if (tile0 < tile1) {
+        if (k == 1 && a.has_pre) tile_barrier();     // the shared tokens' tiles have been read
+#pragma unroll
+        for (int j = 0; j < 3; ++j)
+          if (tile0 + j < tile1) load_tables(tile0 + j);
+        if (TAB) wait_loads<0>();
+        load_k(tile0);
+        if (tile0 + 1 < tile1) load_k(tile0 + 1);
+        load_v(tile0);
+        if (tile0 + 3 < tile1) load_tables(tile0 + 3);
+        if (tile0 + 1 < tile1) {
+          if (tile0 + 2 < tile1) load_k(tile0 + 2);
+          load_v(tile0 + 1);
+        }
+        // What the compiler loaded has to have arrived before the loop, or its own
+        // waits inside would drain the tiles under way.
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qf[ks]));
+        asm volatile("" : "+v"(qp));
+        f32x16 xa[2], xb[2];
+        float ma, mb;
+        // under way, oldest first: step t, tables(t + 3), step t + 1
+        auto turn = [&](int t, bool first, f32x16 (&x)[2], float& mx, f32x16 (&y)[2], float& my) {
+          if (t + 3 < tile1) wait_loads<T + KV>();
+          else if (t + 2 < tile1) wait_loads<KV>();
+          else if (t + 1 < tile1) wait_loads<L::LOADS>();
+          else wait_loads<0>();
+          tile_barrier();             // step t is there, and no wave reads step t - 1 any more
+          if (first && wave_on) {
+            score(t, x);
+            mask(t, x);
+            mx = -INFINITY;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) mx = max3(mx, x[0][r], x[1][r]);
+          }
+          if (first) tile_barrier();  // K of the first tile has been read
+          if (t + 2 < tile1) {
+            if (t + 4 < tile1) {
+              load_tables(t + 4);
+              wait_loads<KV + T>();
+            } else if (t + 3 < tile1) {
+              wait_loads<KV>();
+            }
+            if (t + 3 < tile1) load_k(t + 3);
+            load_v(t + 2);
+          }
+          if (wave_on) step(t, x, mx, y, my);
+        };
+        turn(tile0, true, xa, ma, xb, mb);
+        for (int t = tile0 + 1; t < tile1; t += 2) {
+          turn(t, false, xb, mb, xa, ma);
+          if (t + 1 < tile1) turn(t + 1, false, xa, ma, xb, mb);
         }
       }
     }
-    const int i = (wave * RW + w) * 32 + c;
-    if (i >= n_rows) continue;
-    if (!PRE && splits == 1 && !a.has_pre) {
+    wait_loads<0>();
+
+    // What follows the tiles finds its lane, row and query again: kept through
+    // the tiles, they would not fit the registers.
+    int ln = lane;
+    asm volatile("" : "+v"(ln));
+    const int c2 = ln & 31, hf2 = ln >> 5, row = wave * 32 + c2;
+    l = sum32(l);
+    if (hidden) {
+      // A token that only some rows of the block see has weight 0 in the others,
+      // and 0 times a value that is not finite is NaN: then the share's tokens
+      // are taken again one by one, each by the rows that see it.
+      bool bad = !__builtin_isfinite(l);
 #pragma unroll
       for (int db = 0; db < DB; ++db)
 #pragma unroll
-        for (int r = 0; r < 16; r += 4)
-          store_row<D, F16>(a, r0, rb * L::kRows + i, g, 32 * db + 2 * r + 4 * hf,
-                            f32x4{o[w][db][r], o[w][db][r + 1], o[w][db][r + 2], o[w][db][r + 3]}, m[w], l[w]);
-    } else {
-      const int64_t at = (int64_t)blockIdx.x * L::kRows + i;
+        for (int r = 0; r < 16; ++r) bad |= !__builtin_isfinite(o[db][r]);
+      if (__ballot(bad) != 0ull) {
+#pragma unroll
+        for (int db = 0; db < DB; ++db) o[db] = zero16();
+        m = -INFINITY;
+        l = 0.f;
+        for (int k = a.has_pre ? 0 : 1; k < (PRE ? 1 : 2); ++k) {
+          const SeqCaches& kv = caches(k);
+          const Part pt = open(k);
+          const int64_t head = g * kv.head_stride + (kv.slot ? 0 : pt.sq * kv.seq_stride);
+          for (int u = pt.tile0 * kTok; u < min(pt.tile1 * kTok, pt.rg.cnt); ++u) {
+            const int t = pt.rg.token(u);
+            const int row = kv.slot ? (int)min((uint32_t)kv.slot[pt.sq * kv.slot_stride + t], (uint32_t)kv.pool_last) : t;
+            const int64_t at = head + row * kv.tok_stride;
+            float x = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+              const u32x4 kk = ldg_u4(kv.k + at + 16 * ks + 8 * hf2);
+#pragma unroll
+              for (int j = 0; j < 8; ++j) x = fmaf(elem<F16>(chunk_elem(kk, j)), elem<F16>(chunk_elem(qf[ks], j)), x);
+            }
+            x = sum32(x) * a.sl2;
+            if (!(t < pt.row_hi && (t >= pt.row_lo || t < pt.rg.n_first))) continue;
+            const float nm = fmaxf(m, x), ref = nm == -INFINITY ? 0.f : nm;
+            const float al = __builtin_amdgcn_exp2f(m - ref), w = __builtin_amdgcn_exp2f(x - ref);
+            m = nm;
+            l = l * al + w;
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+              for (int r = 0; r < 16; ++r)
+                o[db][r] = fmaf(w, elem<F16>(kv.v[at + 32 * db + 8 * (r / 4) + 4 * hf2 + r % 4]), o[db][r] * al);
+          }
+        }
+      }
+    }
+
+    if (PRE || x0 > 0 || x1 < work) {
+      // partial sums: an opening share continues a block that another began
+      const bool goes_on = !PRE && opening && x0 > 0;
+      const int64_t item = PRE ? (int64_t)blockIdx.x : 2 * (int64_t)blockIdx.x + (goes_on ? 0 : 1);
+      if (goes_on) record.w = x1 < work ? 1 : 2;
+      else record = make_int4(s, rb, 1, record.w);
+      if (row < n_rows) {
+        const int64_t at = item * kRB + row;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int r = 0; r < 16; r += 4)
+            *reinterpret_cast<f32x4*>(sp.o + at * D + 32 * db + 2 * r + 4 * hf2) = f32x4{o[db][r], o[db][r + 1], o[db][r + 2], o[db][r + 3]};
+        if (hf2 == 0) *reinterpret_cast<float2*>(sp.ml + at * 2) = make_float2(m, l);
+      }
+      continue;
+    }
+    // A wave's rows go through LDS (its own tenth of the tiles), so that a store
+    // covers whole rows.
+    constexpr int kPitch = 2 * D + 16;
+    static_assert(kNW * 32 * kPitch <= 6 * L::kTileB);
+    tile_barrier();                                  // no wave reads tiles any more
+    char* mine = tiles + wave * 32 * kPitch;
+    if (wave_on) {
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      const float lse = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+      bool bad = l != 0.f && !__builtin_isfinite(lse);
 #pragma unroll
       for (int db = 0; db < DB; ++db)
 #pragma unroll
-        for (int r = 0; r < 16; r += 4)
-          *reinterpret_cast<f32x4*>(sp.o + at * D + 32 * db + 2 * r + 4 * hf) =
-              f32x4{o[w][db][r], o[w][db][r + 1], o[w][db][r + 2], o[w][db][r + 3]};
-      if (hf == 0) {
-        sp.ml[at * 2] = m[w];
-        sp.ml[at * 2 + 1] = l[w];
+        for (int r = 0; r < 16; r += 4) {
+          float y[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            y[j] = l == 0.f ? 0.f : o[db][r + j] * inv;
+            bad |= !__builtin_isfinite(y[j]);
+          }
+          *reinterpret_cast<uint2*>(mine + c2 * kPitch + (32 * db + 2 * r + 4 * hf2) * 2) =
+              make_uint2(pack2<F16>(y[0], y[1]), pack2<F16>(y[2], y[3]));
+        }
+      if (bad && row < n_rows) latch_nonfinite(a.nonfinite);
+      if (a.lse && hf2 == 0 && row < n_rows) {
+        const int q = rb * kRB + row;
+        a.lse[(int64_t)(r0 + q / a.group) * a.Hq + g * a.group + q % a.group] = lse;
+      }
+      wait_lds_reads();                              // the wave's own writes, too
+#pragma unroll
+      for (int j = 0; j < 32 / L::LANES; ++j) {
+        const int r = j * L::LANES + ln / L::CH, ch2 = ln % L::CH, gr = wave * 32 + r;
+        if (gr < n_rows) {
+          const int q = rb * kRB + gr;
+          const int64_t out = (int64_t)(r0 + q / a.group) * a.Hq + g * a.group + q % a.group;
+          *reinterpret_cast<u32x4*>(a.o + out * D + ch2 * 8) = *reinterpret_cast<const u32x4*>(mine + r * kPitch + ch2 * 16);
+        }
       }
     }
   }
+  if (!PRE && !whole && sp.share && tid == 0) sp.share[blockIdx.x] = record;
 }
 
-// The splits of the many-rows kernel, and the shared tokens, joined: a
-// workgroup takes one row block of a KV head (those that finished alone and
-// share nothing are left).
-template <int D, bool F16, int RB>
-__global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, SplitSpace sp, int target, int min_chunk, PrefixParts pp) {
-  __shared__ ItemShared ish;
-  const int g = blockIdx.x % a.Hkv;
-  const Item it = find_item<256, RB>(a, blockIdx.x / a.Hkv, target, min_chunk, ish);
-  if (it.s < 0 || it.split != 0 || (it.n_split == 1 && pp.n_split == 0)) return;
-  const int r0 = row_start(a, it.s), R = row_start(a, it.s + 1) - r0;
-  const int n_rows = min(RB, R * a.group - it.rb * RB);
+// Blocks that fell into several shares: the one that share e began and left (its
+// record: s, rb, 1), with what the shares after it added (w: 1 and on, 2 done).
+template <int D, bool F16>
+__global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, SplitSpace sp, int W) {
+  const int g = blockIdx.x % a.Hkv, e = blockIdx.x / a.Hkv;
+  const int4 began = sp.share[blockIdx.x];
+  if (!began.z) return;
+  int n = 1;
+  for (int w = 1; w == 1 && e + n < W; ++n) w = sp.share[(int64_t)(e + n) * a.Hkv + g].w;
+  const int r0 = row_start(a, began.x), R = row_start(a, began.x + 1) - r0;
+  const int n_rows = min(kRB, R * a.group - began.y * kRB);
   constexpr int TPR = D / 4;
-  const int lead = (r0 - row_start(a, 0)) * a.group + it.rb * RB;
   for (int i = blockIdx.y * 256 + threadIdx.x; i < n_rows * TPR; i += gridDim.y * 256) {
     const int row = i / TPR, w4 = (i % TPR) * 4;
     Joined j = {-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f}};
-    j.template add_all<16>(it.n_split, [&](int k, float& m, float& l, f32x4& o) {
-      const int64_t at = ((int64_t)blockIdx.x + (int64_t)k * a.Hkv) * RB + row;
+    j.template add_all<4>(n, [&](int k, float& m, float& l, f32x4& o) {
+      const int64_t item = 2 * ((int64_t)(e + k) * a.Hkv + g) + (k ? 0 : 1), at = item * kRB + row;
       const float2 ml = *reinterpret_cast<const float2*>(sp.ml + at * 2);
       m = ml.x;
       l = ml.y;
       o = *reinterpret_cast<const f32x4*>(sp.o + at * D + w4);
     });
-    if (pp.n_split) add_prefix(a, pp, D, lead + row, g, w4, j);
-    store_row<D, F16>(a, r0, it.rb * RB + row, g, w4, j.acc, j.m, j.l);
+    store_row<D, F16>(a, r0, began.y * kRB + row, g, w4, j.acc, j.m, j.l);
   }
 }
 
-constexpr int kRW = 1, kNW = 8, kRB = 32 * kRW * kNW;
-
 }  // namespace
 
-AttendPlan plan_wide(const AttendArgs& a, int64_t max_tokens, bool room) {
+AttendPlan plan_wide(const AttendArgs& a, bool room) {
   AttendPlan p;
   p.rows = kRB;
-  p.wide = false;
-  const int64_t n_seq = std::min(a.own.n_seq, a.n_rows);
-  const int64_t blocks = (int64_t)a.n_rows * a.group / kRB + n_seq;     // row blocks of a KV head, at most
-  p.target = 512;
-  p.min_chunk = 256;
-  int64_t e = p.target / a.Hkv + blocks + 1;
-  if (!room || max_tokens <= p.min_chunk || blocks * a.Hkv >= p.target) {
-    p.min_chunk = INT_MAX;                                              // no splits
-    e = blocks;
-  }
-  p.items = e * a.Hkv;
-  p.split = p.min_chunk != INT_MAX;
+  p.alone = false;
+  p.min_chunk = 0;
+  p.target = std::max(1, 256 / a.Hkv);             // a workgroup a compute unit
+  p.blocks = (int64_t)a.n_rows * a.group / kRB + std::min(a.own.n_seq, a.n_rows);   // of a head, at most
+  p.items = 2 * (int64_t)p.target * a.Hkv;
+  p.split = room && p.target > 1;
   return p;
 }
 
@@ -541,38 +774,34 @@ PrefixPlan plan_prefix(const AttendArgs& a) {
   return p;
 }
 
-#define CKV_WIDE(D, F16, TAB, PRE, GRID, K) \
-  attend_wide_kernel<D, F16, TAB, kRW, kNW, PRE><<<GRID, 64 * kNW, 0, s>>>(a, sp, target, min_chunk, K)
-#define CKV_WIDE3(D, F16, PRE, GRID, K) \
-  if (tab) CKV_WIDE(D, F16, true, PRE, GRID, K); \
-  else CKV_WIDE(D, F16, false, PRE, GRID, K)
-#define CKV_WIDE2(PRE, GRID, K) \
+#define CKV_WIDE(D, F16, TAB, PRE, GRID, W, K) attend_wide_kernel<D, F16, TAB, PRE><<<GRID, kNT, 0, s>>>(a, sp, W, K)
+#define CKV_WIDE3(D, F16, PRE, GRID, W, K) \
+  if (tab) CKV_WIDE(D, F16, true, PRE, GRID, W, K); \
+  else CKV_WIDE(D, F16, false, PRE, GRID, W, K)
+#define CKV_WIDE2(PRE, GRID, W, K) \
   if (a.D == 64) { \
-    if (a.f16) { CKV_WIDE3(64, true, PRE, GRID, K); } else { CKV_WIDE3(64, false, PRE, GRID, K); } \
+    if (a.f16) { CKV_WIDE3(64, true, PRE, GRID, W, K); } else { CKV_WIDE3(64, false, PRE, GRID, W, K); } \
   } else { \
-    if (a.f16) { CKV_WIDE3(128, true, PRE, GRID, K); } else { CKV_WIDE3(128, false, PRE, GRID, K); } \
+    if (a.f16) { CKV_WIDE3(128, true, PRE, GRID, W, K); } else { CKV_WIDE3(128, false, PRE, GRID, W, K); } \
   }
 
 hipError_t launch_attend_wide(const AttendArgs& a, const AttendPlan& p, const SplitSpace& sp, hipStream_t s) {
-  const dim3 grid((unsigned)p.items);
-  const bool tab = a.own.slot != nullptr;
-  const int target = p.target, min_chunk = p.min_chunk;
-  CKV_WIDE2(false, grid, 0)
+  const dim3 grid((unsigned)(std::max<int64_t>(p.target, p.blocks) * a.Hkv));
+  const bool tab = a.own.slot || (a.has_pre && a.pre.slot);
+  CKV_WIDE2(false, grid, p.target, p.split ? 0 : 1)
   return hipGetLastError();
 }
 
 hipError_t launch_attend_prefix(const AttendArgs& a, const PrefixPlan& p, const SplitSpace& sp, hipStream_t s) {
   const dim3 grid((unsigned)(p.blocks * p.n_split * a.Hkv));
   const bool tab = a.pre.slot != nullptr;
-  const int target = 0, min_chunk = 0;
-  CKV_WIDE2(true, grid, p.n_split)
+  CKV_WIDE2(true, grid, 0, p.n_split)
   return hipGetLastError();
 }
 
-hipError_t launch_attend_join(const AttendArgs& a, const AttendPlan& p, const SplitSpace& sp, const PrefixParts& pp,
-                              hipStream_t s) {
-  const dim3 grid((unsigned)p.items, 4);
-#define CKV_JOIN(D, F16) attend_join_kernel<D, F16, kRB><<<grid, 256, 0, s>>>(a, sp, p.target, p.min_chunk, pp)
+hipError_t launch_attend_join(const AttendArgs& a, const AttendPlan& p, const SplitSpace& sp, hipStream_t s) {
+  const dim3 grid((unsigned)(p.target * a.Hkv), 8);
+#define CKV_JOIN(D, F16) attend_join_kernel<D, F16><<<grid, 256, 0, s>>>(a, sp, p.target)
   if (a.D == 64) {
     if (a.f16) CKV_JOIN(64, true);
     else CKV_JOIN(64, false);

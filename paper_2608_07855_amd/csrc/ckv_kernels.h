@@ -410,6 +410,7 @@ struct SplitSpace {
   float* o;        // [items][rows][D], weighted values against the largest logit
   float* ml;       // [items][rows][2]: that logit (log2 units), the sum of the weights
   int* arrive;     // few-rows kernel: [items], zero between calls
+  int4* share;     // many-rows kernel: [workgroups], what each left of blocks that it shares (or null)
 };
 
 // Partial sums over the shared tokens by packed row (all sequences' rows of a
@@ -420,16 +421,17 @@ struct PrefixParts {
   int n_split, block_rows;   // n_split 0: none
 };
 
-// How a call is cut into items (row blocks of `rows` rows and splits); room:
-// whether there may be partial sums.  split: whether there are.
+// How a call is cut into items of `rows` rows; room: whether there may be
+// partial sums.  split: whether there are.  Many rows: `target` equal shares a
+// KV head, at most two partial row blocks each.
 struct AttendPlan {
-  int64_t items;
+  int64_t items, blocks;
   int rows, target, min_chunk;
   bool split;
-  bool wide;       // few-rows kernel: workgroups that take a compute unit each
+  bool alone;      // few-rows kernel: workgroups that take a compute unit each
 };
 AttendPlan plan_narrow(const AttendArgs& a, int64_t max_tokens, bool room);
-AttendPlan plan_wide(const AttendArgs& a, int64_t max_tokens, bool room);
+AttendPlan plan_wide(const AttendArgs& a, bool room);
 struct PrefixPlan {
   int64_t blocks;
   int rows, n_split;
@@ -439,11 +441,12 @@ PrefixPlan plan_prefix(const AttendArgs& a);
 // Few rows: finished in one launch (with the prefix's partial sums joined).
 hipError_t launch_attend_narrow(const AttendArgs& a, const AttendPlan& p, const SplitSpace& sp, const PrefixParts& pp,
                                 hipStream_t s);
-// Many rows: what is split or shares a prefix is finished by launch_attend_join.
+// Many rows, shared tokens first; blocks that were split are finished by
+// launch_attend_join.  launch_attend_prefix: the shared tokens alone, for the
+// few-rows kernel.
 hipError_t launch_attend_wide(const AttendArgs& a, const AttendPlan& p, const SplitSpace& sp, hipStream_t s);
 hipError_t launch_attend_prefix(const AttendArgs& a, const PrefixPlan& p, const SplitSpace& sp, hipStream_t s);
-hipError_t launch_attend_join(const AttendArgs& a, const AttendPlan& p, const SplitSpace& sp, const PrefixParts& pp,
-                              hipStream_t s);
+hipError_t launch_attend_join(const AttendArgs& a, const AttendPlan& p, const SplitSpace& sp, hipStream_t s);
 
 struct SlotArgs {
   int n_seq, block_size, n_blocks, max_new;
