@@ -1751,6 +1751,7 @@ int check_batch(ckv_ctx* c, const ckv_batch_view* kv, const char* what) {
     return fail(c, CKV_ERR_ARG, "%s: K/V rows must be 16-byte aligned (strides multiples of 8)", what);
   if (kv->tok_stride < kv->head_dim || kv->head_stride < 0 || (!kv->slot && kv->seq_stride < 0))
     return fail(c, CKV_ERR_SHAPE, "%s: K/V strides too small", what);
+  if (kv->tok_stride > INT_MAX) return fail(c, CKV_ERR_UNSUPPORTED, "%s: tok_stride must stay below 2^31 elements", what);
   if (kv->slot && kv->pool_rows < 1) return fail(c, CKV_ERR_SHAPE, "%s: a paged view needs pool_rows >= 1", what);
   if (kv->n_seq > 1 && ((kv->slot && kv->slot_stride < kv->max_tokens) || (kv->pos && kv->pos_stride < kv->max_tokens)))
     return fail(c, CKV_ERR_SHAPE, "%s: slot and pos rows must hold max_tokens entries", what);

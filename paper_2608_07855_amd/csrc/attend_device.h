@@ -11,6 +11,12 @@ namespace ckv {
 
 namespace {
 
+// the same in every lane
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ long long uniform(long long x) {
+  return (long long)((unsigned long long)(unsigned)uniform((int)x) | (unsigned long long)(unsigned)uniform((int)(x >> 32)) << 32);
+}
+
 __device__ __forceinline__ int clampi(int x, int lo, int hi) { return min(max(x, lo), hi); }
 
 __device__ __forceinline__ int seq_tokens(const SeqCaches& c, int s) { return clampi(c.n_tokens[s], 0, c.max_tokens); }
@@ -277,6 +283,11 @@ __device__ __forceinline__ uint32_t lds_at(const void* p) {
 }
 __device__ __forceinline__ void load_lds16(const void* g, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(g) : "memory");
+}
+// the same at a 32-bit offset from an address that the wave shares
+__device__ __forceinline__ void load_lds16_near(const void* g, uint32_t offset, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(lds)),
+               "v"(offset), "s"(uniform((long long)(uintptr_t)g)) : "memory");
 }
 __device__ __forceinline__ void load_lds4(const void* g, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(g) : "memory");

@@ -36,7 +36,8 @@ namespace {
 // ---------------------------------------------------------------------------
 constexpr float kLag = 8.f;   // log2 units
 constexpr int kAhead = 4;     // operands read from LDS ahead of their products
-constexpr int kNW = 8, kNT = 64 * kNW, kRB = 32 * kNW, kTok = 64;
+constexpr int kRW = 1;        // 32-row blocks of a wave
+constexpr int kNW = 8 / kRW, kNT = 64 * kNW, kRB = 256, kTok = 64;
 
 template <int D>
 struct Wide {
@@ -68,12 +69,6 @@ __device__ __forceinline__ uint32_t pack2(float x, float y) {
 }
 
 __device__ __forceinline__ void tile_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
-
-// the same in every lane
-__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ __forceinline__ long long uniform(long long x) {
-  return (long long)((unsigned long long)(unsigned)uniform((int)x) | (unsigned long long)(unsigned)uniform((int)(x >> 32)) << 32);
-}
 
 // ---------------------------------------------------------------- shares
 
@@ -230,19 +225,35 @@ struct Part {
   Range rg;
   int n, base, sq, tile0, tile1;
   int full_lo, full_hi;   // tokens that every row of the wave sees: [full_lo, full_hi), and first ones before full_hi
-  int row_lo, row_hi;     // tokens that the lane's row sees: [row_lo, row_hi), and first ones before row_hi
+  int row_lo[kRW], row_hi[kRW];   // tokens that the lane's rows see: [row_lo, row_hi), and first ones before row_hi
 };
+
+// The kernel's first argument, read from memory where it is used next.
+__device__ __forceinline__ const AttendArgs& fresh_args(const AttendArgs&) {
+  typedef const __attribute__((address_space(4))) AttendArgs* Ptr;
+  Ptr p = (Ptr)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return *(const AttendArgs*)p;
+}
+
+enum Kept { kS, kRb, kR0, kRows, kX0, kX1 = kX0 + 2, kWork = kX1 + 2, kQmin = kWork + 2, kQmax, kBmin, kBmax, kNextS, kNextRb,
+            kNextX, kLeft = kNextX + 2, kOpening = kLeft + 2, kRecord };
 
 // PRE: the rows of all sequences over the shared tokens, in n_split splits, as
 // partial sums.  Otherwise a share of the blocks (W shares a KV head), in each
 // the shared tokens first; n_split 1: whole blocks only.
 template <int D, bool F16, bool TAB, bool PRE>
-__global__ __launch_bounds__(kNT) void attend_wide_kernel(AttendArgs a, SplitSpace sp, int W, int n_split) {
+__global__ __launch_bounds__(kNT, 2 / kRW) void attend_wide_kernel(AttendArgs args, SplitSpace sp, int W, int n_split) {
   using L = Wide<D>;
   constexpr int KS = D / 16, DB = D / 32;
   __shared__ __align__(256) char tiles[L::kLds];
   __shared__ ShareShared ssh;
   __shared__ int qlim[2][kNW];
+  // What a block needs again behind its tiles waits in LDS (a copy a wave), and
+  // the arguments are read anew: kept in scalar registers through the tiles they
+  // spill, and a spilled register's reload inside the loop drains the loads.
+  __shared__ volatile int kept[kNW][32];
+  const AttendArgs& a = fresh_args(args);
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), c = lane & 31, hf = lane >> 5;
   const int g = blockIdx.x % a.Hkv, e = blockIdx.x / a.Hkv;
   const int pre_n = a.has_pre ? uniform(seq_tokens(a.pre, 0)) : 0;
@@ -279,9 +290,19 @@ __global__ __launch_bounds__(kNT) void attend_wide_kernel(AttendArgs a, SplitSpa
     }
     if (me.s < 0) return;
   }
+  auto keep = [&](int i, int v) {
+    if (lane == 0) kept[wave][i] = v;
+  };
+  auto keep64 = [&](int i, long long v) {
+    keep(i, (int)v);
+    keep(i + 1, (int)(v >> 32));
+  };
+  auto get = [&](int i) { return uniform(kept[wave][i]); };
+  auto get64 = [&](int i) { return (long long)((unsigned long long)(unsigned)get(i) | (unsigned long long)(unsigned)get(i + 1) << 32); };
   int4 record = make_int4(0, 0, 0, 0);
   for (bool opening = true; me.left > 0; opening = false) {
     if (!opening) tile_barrier();          // the block before is done with LDS
+    const AttendArgs& a = fresh_args(args);
     // the share's part of this block
     const int s = me.s, rb = me.rb;
     const int r0 = uniform(row_start(a, PRE ? 0 : s)), R = uniform(row_start(a, PRE ? a.own.n_seq : s + 1)) - r0;
@@ -305,22 +326,26 @@ __global__ __launch_bounds__(kNT) void attend_wide_kernel(AttendArgs a, SplitSpa
       me.left = 0;
     }
 
-    // the lane's row: its position and query
-    const int i = min(wave * 32 + c, n_rows - 1);
-    const int rr = rb * kRB + i, p = rr / a.group, h = g * a.group + rr % a.group;
-    int qp;
-    if constexpr (PRE) {
-      const int row = r0 + p, rs = max(row_seq(a, row), 0), f = row_start(a, rs);
-      qp = row_position(a, rs, f, row_start(a, rs + 1) - f, row - f, seq_tokens(a.own, rs), pre_n);
-    } else {
-      qp = row_position(a, s, r0, R, p, seq_tokens(a.own, s), pre_n);
-    }
-    u32x4 qf[KS];
-    const uint16_t* qr = a.q + (int64_t)(r0 + p) * a.q_row_stride + (int64_t)h * a.q_head_stride;
+    // the lane's rows: their positions and queries
+    int qp[kRW], qmin = INT_MAX, qmax = INT_MIN;
+    u32x4 qf[kRW][KS];
+    const bool wave_on = wave * 32 * kRW < n_rows;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) qf[ks] = ldg_u4(qr + 16 * ks + 8 * hf);
-    const bool wave_on = wave * 32 < n_rows;
-    int qmin = qp, qmax = qp;
+    for (int w = 0; w < kRW; ++w) {
+      const int i = min((wave * kRW + w) * 32 + c, n_rows - 1);
+      const int rr = rb * kRB + i, p = rr / a.group, h = g * a.group + rr % a.group;
+      if constexpr (PRE) {
+        const int row = r0 + p, rs = max(row_seq(a, row), 0), f = row_start(a, rs);
+        qp[w] = row_position(a, rs, f, row_start(a, rs + 1) - f, row - f, seq_tokens(a.own, rs), pre_n);
+      } else {
+        qp[w] = row_position(a, s, r0, R, p, seq_tokens(a.own, s), pre_n);
+      }
+      const uint16_t* qr = a.q + (int64_t)(r0 + p) * a.q_row_stride + (int64_t)h * a.q_head_stride;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) qf[w][ks] = ldg_u4(qr + 16 * ks + 8 * hf);
+      qmin = min(qmin, qp[w]);
+      qmax = max(qmax, qp[w]);
+    }
 #pragma unroll
     for (int off = 16; off; off >>= 1) {
       qmin = min(qmin, __shfl_xor(qmin, off, 64));
@@ -337,20 +362,42 @@ __global__ __launch_bounds__(kNT) void attend_wide_kernel(AttendArgs a, SplitSpa
       bmin = min(bmin, qlim[0][w]);
       bmax = max(bmax, qlim[1][w]);
     }
-    qmin = uniform(qmin);
-    qmax = uniform(qmax);
-    bmin = uniform(bmin);
-    bmax = uniform(bmax);
+    keep(kS, s);
+    keep(kRb, rb);
+    keep(kR0, r0);
+    keep(kRows, n_rows);
+    keep64(kX0, x0);
+    keep64(kX1, x1);
+    keep64(kWork, work);
+    keep(kQmin, qmin);
+    keep(kQmax, qmax);
+    keep(kBmin, bmin);
+    keep(kBmax, bmax);
+    keep(kNextS, me.s);
+    keep(kNextRb, me.rb);
+    keep64(kNextX, me.x);
+    keep64(kLeft, me.left);
+    keep(kOpening, opening);
+    keep(kRecord, record.x);
+    keep(kRecord + 1, record.y);
+    keep(kRecord + 2, record.z);
+    keep(kRecord + 3, record.w);
 
-    f32x16 o[DB];
-    float m = -INFINITY, l = 0.f;
+    f32x16 o[kRW][DB];
+    float m[kRW], l[kRW];
 #pragma unroll
-    for (int db = 0; db < DB; ++db) o[db] = zero16();
+    for (int w = 0; w < kRW; ++w) {
+      m[w] = -INFINITY;
+      l[w] = 0.f;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) o[w][db] = zero16();
+    }
     bool hidden = false;          // some tile held tokens that not all rows see
 
-    auto caches = [&](int k) -> const SeqCaches& { return k ? a.own : a.pre; };
     auto open = [&](int k) {
-      const SeqCaches& kv = caches(k);
+      const AttendArgs& a = fresh_args(args);
+      const SeqCaches& kv = k ? a.own : a.pre;
+      const int s = get(kS), qmin = get(kQmin), qmax = get(kQmax), bmin = get(kBmin), bmax = get(kBmax);
       Part t;
       t.sq = k ? s : 0;
       t.n = uniform(seq_tokens(kv, t.sq));
@@ -376,12 +423,18 @@ __global__ __launch_bounds__(kNT) void attend_wide_kernel(AttendArgs a, SplitSpa
           }
           return lo;
         };
-        t.row_hi = find(t.full_hi, t.rg.hi, qp);
-        t.row_lo = a.window ? find(t.rg.lo, t.rg.hi, (long long)qp - a.window) : 0;
+#pragma unroll
+        for (int w = 0; w < kRW; ++w) {
+          t.row_hi[w] = find(t.full_hi, t.rg.hi, qp[w]);
+          t.row_lo[w] = a.window ? find(t.rg.lo, t.rg.hi, (long long)qp[w] - a.window) : 0;
+        }
       } else {
         auto in = [&](long long x) { return (int)min(max(x, 0ll), (long long)t.n); };
-        t.row_hi = in((long long)qp + 1 - t.base);
-        t.row_lo = a.window ? in((long long)qp - a.window + 1 - t.base) : 0;
+#pragma unroll
+        for (int w = 0; w < kRW; ++w) {
+          t.row_hi[w] = in((long long)qp[w] + 1 - t.base);
+          t.row_lo[w] = a.window ? in((long long)qp[w] - a.window + 1 - t.base) : 0;
+        }
       }
       const int n_tiles = (t.rg.cnt + kTok - 1) / kTok;
       if constexpr (PRE) {
@@ -389,87 +442,109 @@ __global__ __launch_bounds__(kNT) void attend_wide_kernel(AttendArgs a, SplitSpa
         t.tile0 = min(split * per, n_tiles);
         t.tile1 = min(t.tile0 + per, n_tiles);
       } else {
-        const long long from = k ? pre_n : 0, len = k ? work - pre_n : pre_n;
-        t.tile0 = uniform(tile_at(x0 - from, len, n_tiles));
-        t.tile1 = uniform(tile_at(x1 - from, len, n_tiles));
+        const long long from = k ? pre_n : 0, len = k ? get64(kWork) - pre_n : pre_n;
+        t.tile0 = uniform(tile_at(get64(kX0) - from, len, n_tiles));
+        t.tile1 = uniform(tile_at(get64(kX1) - from, len, n_tiles));
       }
       return t;
     };
 
-    for (int k = a.has_pre ? 0 : 1; k < (PRE ? 1 : 2); ++k) {
-      const SeqCaches& kv = caches(k);
+    const bool has_pre = a.has_pre;
+    for (int k = has_pre ? 0 : 1; k < (PRE ? 1 : 2); ++k) {
+      const AttendArgs& a = fresh_args(args);
+      const SeqCaches& kv = k ? a.own : a.pre;
       const Part pt = open(k);
+      const float sl2 = a.sl2;
       const Range rg = pt.rg;
       const int tile0 = pt.tile0, tile1 = pt.tile1;
       const int64_t head = g * kv.head_stride + (kv.slot ? 0 : pt.sq * kv.seq_stride);
       const char* kh = reinterpret_cast<const char*>(kv.k + head);
       const char* vh = reinterpret_cast<const char*>(kv.v + head);
       const int32_t* slots = kv.slot ? kv.slot + pt.sq * kv.slot_stride : nullptr;
-      const int64_t row_bytes = kv.tok_stride * 2;
+      const uint32_t row_bytes = (uint32_t)kv.tok_stride * 2;
+      // rows that 32-bit offsets reach (24-bit products) take one instruction each
+      const int last_row = slots ? kv.pool_last : max(pt.n - 1, 0);
+      const bool near = (uint64_t)last_row * row_bytes + row_bytes < (1ull << 32) && last_row < (1 << 24) && row_bytes < (1u << 24);
       auto token = [&](int tile, int r) { return rg.token(min(tile * kTok + r, rg.cnt - 1)); };
       // (where only the other part has a table, any word keeps the count of loads)
       auto load_tables = [&](int tile) {
         if constexpr (TAB)
           load_lds4(slots ? slots + token(tile, wave * L::kOwn + lane % L::kOwn) : a.cu_rows, tab + (tile & 3) * 256);
       };
-      auto row_offset = [&](int tile, int j) -> int64_t {
-        int row;
-        if (TAB && slots) {
-          const auto* w = (const __attribute__((address_space(3))) int*)(uintptr_t)(tab + (tile & 3) * 256);
-          row = (int)min((uint32_t)w[j * L::LANES + grp], (uint32_t)kv.pool_last);
-        } else {
-          row = token(tile, wave * L::kOwn + j * L::LANES + grp);
+      auto find_rows = [&](int tile, uint32_t (&rows)[L::LOADS]) {
+#pragma unroll
+        for (int j = 0; j < L::LOADS; ++j) {
+          if (TAB && slots) {
+            const auto* w = (const __attribute__((address_space(3))) int*)(uintptr_t)(tab + (tile & 3) * 256);
+            rows[j] = min((uint32_t)w[j * L::LANES + grp], (uint32_t)kv.pool_last);
+          } else {
+            rows[j] = token(tile, wave * L::kOwn + j * L::LANES + grp);
+          }
         }
-        return row * row_bytes;
       };
       // K (at lane constant kc) or V of a tile; load j's rows are LANES j further
-      auto load_rows = [&](int tile, const char* from, uint32_t lane_c, uint32_t step_c, uint32_t to) {
-        int64_t at[L::LOADS];
-#pragma unroll
-        for (int j = 0; j < L::LOADS; ++j) at[j] = row_offset(tile, j);
+      auto load_rows = [&](const uint32_t (&rows)[L::LOADS], const char* from, uint32_t lane_c, uint32_t step_c, uint32_t to) {
         wait_lds_reads();
         // (opaque, or the compiler keeps a 64-bit sum for every load in registers)
         asm volatile("" : "+v"(lane_c));
+        if (near) {
 #pragma unroll
-        for (int j = 0; j < L::LOADS; ++j)
-          load_lds16(from + (at[j] + (lane_c ^ (j * step_c))), to + (wave * L::LOADS + j) * 1024);
+          for (int j = 0; j < L::LOADS; ++j)
+            load_lds16_near(from, __umul24(rows[j], row_bytes) + (lane_c ^ (j * step_c)), to + (wave * L::LOADS + j) * 1024);
+        } else {
+#pragma unroll
+          for (int j = 0; j < L::LOADS; ++j)
+            load_lds16(from + ((uint64_t)rows[j] * row_bytes + (lane_c ^ (j * step_c))), to + (wave * L::LOADS + j) * 1024);
+        }
       };
-      auto load_k = [&](int tile) { load_rows(tile, kh, kc, (L::LANES & (L::CH - 1)) << 4, lds + (tile % 3) * L::kTileB); };
-      auto load_v = [&](int tile) {
-        load_rows(tile, vh, vc, (2 * L::LANES & (L::CH - 1)) << 4, lds + (3 + tile % 3) * L::kTileB);
+      auto load_k = [&](int tile, const uint32_t (&rows)[L::LOADS]) {
+        load_rows(rows, kh, kc, (L::LANES & (L::CH - 1)) << 4, lds + (tile % 3) * L::kTileB);
+      };
+      auto load_v = [&](int tile, const uint32_t (&rows)[L::LOADS]) {
+        load_rows(rows, vh, vc, (2 * L::LANES & (L::CH - 1)) << 4, lds + (3 + tile % 3) * L::kTileB);
       };
 
       // scores of a tile (raw products)
-      auto score = [&](int tile, f32x16 (&x)[2]) {
+      auto score = [&](int tile, f32x16 (&x)[kRW][2]) {
         const uint32_t off = (tile % 3) * L::kTileB;
 #pragma unroll
         for (int tb = 0; tb < 2; ++tb) {
-          x[tb] = zero16();
 #pragma unroll
-          for (int ks = 0; ks < KS; ++ks) x[tb] = mfma32<F16>(lds_read16((ka + off) ^ (32 * ks), tb * 32 * L::kRowB), qf[ks], x[tb]);
+          for (int w = 0; w < kRW; ++w) x[w][tb] = zero16();
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) {
+            const u32x4 kf = lds_read16((ka + off) ^ (32 * ks), tb * 32 * L::kRowB);
+#pragma unroll
+            for (int w = 0; w < kRW; ++w) x[w][tb] = mfma32<F16>(kf, qf[w][ks], x[w][tb]);
+          }
         }
       };
       // hides what a row does not see
-      auto mask = [&](int tile, f32x16 (&x)[2]) {
+      auto mask = [&](int tile, f32x16 (&x)[kRW][2]) {
         const int u0 = tile * kTok, u1 = u0 + kTok - 1, ta = rg.token(u0), te = rg.token(u1);
         if (te < pt.full_hi && (ta >= pt.full_lo || te < rg.n_first)) return;
         hidden = true;
         if (ta >= rg.n_first && u0 >= rg.ns) {
-          const uint32_t len = max(pt.row_hi - pt.row_lo, 0), d = ta + 4 * hf - pt.row_lo;
 #pragma unroll
-          for (int tb = 0; tb < 2; ++tb)
+          for (int w = 0; w < kRW; ++w) {
+            const uint32_t len = max(pt.row_hi[w] - pt.row_lo[w], 0), d = ta + 4 * hf - pt.row_lo[w];
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-              x[tb][r] = d + (uint32_t)(32 * tb + 8 * (r / 4) + r % 4) < len ? x[tb][r] : -INFINITY;
+            for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+              for (int r = 0; r < 16; ++r)
+                x[w][tb][r] = d + (uint32_t)(32 * tb + 8 * (r / 4) + r % 4) < len ? x[w][tb][r] : -INFINITY;
+          }
           return;
         }
 #pragma unroll
-        for (int tb = 0; tb < 2; ++tb)
+        for (int w = 0; w < kRW; ++w)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int t = rg.token(u0 + 32 * tb + 8 * (r / 4) + 4 * hf + r % 4);
-            x[tb][r] = t < pt.row_hi && (t >= pt.row_lo || t < rg.n_first) ? x[tb][r] : -INFINITY;
-          }
+          for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const int t = rg.token(u0 + 32 * tb + 8 * (r / 4) + 4 * hf + r % 4);
+              x[w][tb][r] = t < pt.row_hi[w] && (t >= pt.row_lo[w] || t < rg.n_first) ? x[w][tb][r] : -INFINITY;
+            }
       };
 
       // One step: the weights of tile t from its scores x (largest one of a lane
@@ -477,18 +552,22 @@ __global__ __launch_bounds__(kNT) void attend_wide_kernel(AttendArgs a, SplitSpa
       // the largest of y.  A wave issues in order, so the vector work is written
       // between the products, and operands are read from LDS kAhead products
       // early; the fences keep the compiler from gathering either.
-      auto step = [&](int t, f32x16 (&x)[2], float& mx, f32x16 (&y)[2], float& my) {
-        const float top = max32(mx) * a.sl2;
-        if (__ballot(top > m + kLag || (m == -INFINITY && top > m)) != 0ull) {
-          const float nm = top > m ? top : m;
-          const float al = nm == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - nm);
-          l *= al;
+      auto step = [&](int t, f32x16 (&x)[kRW][2], float (&mx)[kRW], f32x16 (&y)[kRW][2], float (&my)[kRW]) {
+        float ref[kRW];
 #pragma unroll
-          for (int db = 0; db < DB; ++db) o[db] *= al;
-          m = nm;
+        for (int w = 0; w < kRW; ++w) {
+          const float top = max32(mx[w]) * sl2;
+          if (__ballot(top > m[w] + kLag || (m[w] == -INFINITY && top > m[w])) != 0ull) {
+            const float nm = top > m[w] ? top : m[w];
+            const float al = nm == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[w] - nm);
+            l[w] *= al;
+#pragma unroll
+            for (int db = 0; db < DB; ++db) o[w][db] *= al;
+            m[w] = nm;
+          }
+          ref[w] = m[w] == -INFINITY ? 0.f : m[w];
         }
-        const float ref = m == -INFINITY ? 0.f : m;
-        u32x4 ph[4];
+        u32x4 ph[kRW][4];
         {
           // past the last tile: what an older tile left, used by nobody
           const uint32_t off = ((t + 1) % 3) * L::kTileB;
@@ -499,23 +578,29 @@ __global__ __launch_bounds__(kNT) void attend_wide_kernel(AttendArgs a, SplitSpa
           __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
           for (int j = 0; j < 2 * KS; ++j) {
-            y[j % 2] = mfma32<F16>(kf[j % kAhead], qf[j / 2], j < 2 ? zero16() : y[j % 2]);
-            if (j + kAhead < 2 * KS) kf[j % kAhead] = read(j + kAhead);
-            // the tile's 16 pairs of scores, over the 2 KS products
 #pragma unroll
-            for (int q = j * 16 / (2 * KS); q < (j + 1) * 16 / (2 * KS); ++q) {
-              const int tb = q / 8, r = 2 * (q % 8);
-              const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[tb][r], a.sl2, -ref));
-              const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[tb][r + 1], a.sl2, -ref));
-              l += p0 + p1;
-              ph[q / 4][q % 4] = pack2<F16>(p0, p1);
+            for (int w = 0; w < kRW; ++w) {
+              y[w][j % 2] = mfma32<F16>(kf[j % kAhead], qf[w][j / 2], j < 2 ? zero16() : y[w][j % 2]);
+              if (w == kRW - 1 && j + kAhead < 2 * KS) kf[j % kAhead] = read(j + kAhead);
+              // the tile's 16 pairs of scores, over the 2 KS products
+#pragma unroll
+              for (int q = j * 16 / (2 * KS); q < (j + 1) * 16 / (2 * KS); ++q) {
+                const int tb = q / 8, r = 2 * (q % 8);
+                const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[w][tb][r], sl2, -ref[w]));
+                const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[w][tb][r + 1], sl2, -ref[w]));
+                l[w] += p0 + p1;
+                ph[w][q / 4][q % 4] = pack2<F16>(p0, p1);
+              }
+              __builtin_amdgcn_sched_barrier(0);
             }
-            __builtin_amdgcn_sched_barrier(0);
           }
           // keeps the weights here, beside the products
 #pragma unroll
-          for (int j = 0; j < 4; ++j) asm volatile("" : "+v"(ph[j]));
-          asm volatile("" : "+v"(l));
+          for (int w = 0; w < kRW; ++w) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) asm volatile("" : "+v"(ph[w][j]));
+            asm volatile("" : "+v"(l[w]));
+          }
         }
         if (t + 1 < tile1) mask(t + 1, y);
         {
@@ -528,45 +613,61 @@ __global__ __launch_bounds__(kNT) void attend_wide_kernel(AttendArgs a, SplitSpa
           };
 #pragma unroll
           for (int j = 0; j < kAhead; ++j) vf[j] = read(j);
-          my = -INFINITY;
+#pragma unroll
+          for (int w = 0; w < kRW; ++w) my[w] = -INFINITY;
           __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
           for (int j = 0; j < 4 * DB; ++j) {
-            o[j % DB] = mfma32<F16>(vf[j % kAhead], ph[j / DB], o[j % DB]);
-            if (j + kAhead < 4 * DB) vf[j % kAhead] = read(j + kAhead);
 #pragma unroll
-            for (int q = j * 16 / (4 * DB); q < (j + 1) * 16 / (4 * DB); ++q)
-              my = max3(my, y[q / 8][2 * (q % 8)], y[q / 8][2 * (q % 8) + 1]);
-            __builtin_amdgcn_sched_barrier(0);
+            for (int w = 0; w < kRW; ++w) {
+              o[w][j % DB] = mfma32<F16>(vf[j % kAhead], ph[w][j / DB], o[w][j % DB]);
+              if (w == kRW - 1 && j + kAhead < 4 * DB) vf[j % kAhead] = read(j + kAhead);
+#pragma unroll
+              for (int q = j * 16 / (4 * DB); q < (j + 1) * 16 / (4 * DB); ++q)
+                my[w] = max3(my[w], y[w][q / 8][2 * (q % 8)], y[w][q / 8][2 * (q % 8) + 1]);
+              __builtin_amdgcn_sched_barrier(0);
+            }
           }
         }
       };
 
-      // A load step j brings V of tile j and K of tile j + 1; two are under way.
+      // A load step j brings V of tile j and K of tile j + 1 (whose rows the next
+      // step's V has, too); two steps are under way.
       constexpr int KV = 2 * L::LOADS, T = TAB ? 1 : 0;
       if (tile0 < tile1) {
-        if (k == 1 && a.has_pre) tile_barrier();     // the shared tokens' tiles have been read
+        if (k == 1 && has_pre) tile_barrier();     // the shared tokens' tiles have been read
 #pragma unroll
         for (int j = 0; j < 3; ++j)
           if (tile0 + j < tile1) load_tables(tile0 + j);
         if (TAB) wait_loads<0>();
-        load_k(tile0);
-        if (tile0 + 1 < tile1) load_k(tile0 + 1);
-        load_v(tile0);
+        uint32_t rows[L::LOADS], ahead[L::LOADS];
+        find_rows(tile0, rows);
+        load_k(tile0, rows);
+        if (tile0 + 1 < tile1) {
+          find_rows(tile0 + 1, ahead);
+          load_k(tile0 + 1, ahead);
+        }
+        load_v(tile0, rows);
         if (tile0 + 3 < tile1) load_tables(tile0 + 3);
         if (tile0 + 1 < tile1) {
-          if (tile0 + 2 < tile1) load_k(tile0 + 2);
-          load_v(tile0 + 1);
+          if (tile0 + 2 < tile1) {
+            find_rows(tile0 + 2, rows);
+            load_k(tile0 + 2, rows);
+          }
+          load_v(tile0 + 1, ahead);
         }
         // What the compiler loaded has to have arrived before the loop, or its own
         // waits inside would drain the tiles under way.
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qf[ks]));
-        asm volatile("" : "+v"(qp));
-        f32x16 xa[2], xb[2];
-        float ma, mb;
-        // under way, oldest first: step t, tables(t + 3), step t + 1
-        auto turn = [&](int t, bool first, f32x16 (&x)[2], float& mx, f32x16 (&y)[2], float& my) {
+        for (int w = 0; w < kRW; ++w) {
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qf[w][ks]));
+          asm volatile("" : "+v"(qp[w]));
+        }
+        f32x16 xa[kRW][2], xb[kRW][2];
+        float ma[kRW], mb[kRW];
+        // under way, oldest first: step t, tables(t + 3), step t + 1; rows: of tile t + 2
+        auto turn = [&](int t, bool first, f32x16 (&x)[kRW][2], float (&mx)[kRW], f32x16 (&y)[kRW][2], float (&my)[kRW]) {
           if (t + 3 < tile1) wait_loads<T + KV>();
           else if (t + 2 < tile1) wait_loads<KV>();
           else if (t + 1 < tile1) wait_loads<L::LOADS>();
@@ -575,9 +676,12 @@ __global__ __launch_bounds__(kNT) void attend_wide_kernel(AttendArgs a, SplitSpa
           if (first && wave_on) {
             score(t, x);
             mask(t, x);
-            mx = -INFINITY;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) mx = max3(mx, x[0][r], x[1][r]);
+            for (int w = 0; w < kRW; ++w) {
+              mx[w] = -INFINITY;
+#pragma unroll
+              for (int r = 0; r < 16; ++r) mx[w] = max3(mx[w], x[w][0][r], x[w][1][r]);
+            }
           }
           if (first) tile_barrier();  // K of the first tile has been read
           if (t + 2 < tile1) {
@@ -587,8 +691,13 @@ __global__ __launch_bounds__(kNT) void attend_wide_kernel(AttendArgs a, SplitSpa
             } else if (t + 3 < tile1) {
               wait_loads<KV>();
             }
-            if (t + 3 < tile1) load_k(t + 3);
-            load_v(t + 2);
+            if (t + 3 < tile1) {
+              find_rows(t + 3, ahead);
+              load_k(t + 3, ahead);
+            }
+            load_v(t + 2, rows);
+#pragma unroll
+            for (int j = 0; j < L::LOADS; ++j) rows[j] = ahead[j];
           }
           if (wave_on) step(t, x, mx, y, my);
         };
@@ -605,80 +714,93 @@ __global__ __launch_bounds__(kNT) void attend_wide_kernel(AttendArgs a, SplitSpa
     // the tiles, they would not fit the registers.
     int ln = lane;
     asm volatile("" : "+v"(ln));
-    const int c2 = ln & 31, hf2 = ln >> 5, row = wave * 32 + c2;
-    l = sum32(l);
-    if (hidden) {
+    const int c2 = ln & 31, hf2 = ln >> 5;
+    const AttendArgs& b = fresh_args(args);
+    const int s2 = get(kS), rb2 = get(kRb), r2 = get(kR0), rows2 = get(kRows);
+    const bool begun = get64(kX0) > 0, ends = get64(kX1) >= get64(kWork), first = get(kOpening);
+    me = {get(kNextS), get(kNextRb), get64(kNextX), get64(kLeft), false};
+    record = make_int4(get(kRecord), get(kRecord + 1), get(kRecord + 2), get(kRecord + 3));
+#pragma unroll
+    for (int w = 0; w < kRW; ++w) {
+      l[w] = sum32(l[w]);
+      if (!hidden) continue;
       // A token that only some rows of the block see has weight 0 in the others,
       // and 0 times a value that is not finite is NaN: then the share's tokens
       // are taken again one by one, each by the rows that see it.
-      bool bad = !__builtin_isfinite(l);
+      bool bad = !__builtin_isfinite(l[w]);
 #pragma unroll
       for (int db = 0; db < DB; ++db)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) bad |= !__builtin_isfinite(o[db][r]);
-      if (__ballot(bad) != 0ull) {
+        for (int r = 0; r < 16; ++r) bad |= !__builtin_isfinite(o[w][db][r]);
+      if (__ballot(bad) == 0ull) continue;
 #pragma unroll
-        for (int db = 0; db < DB; ++db) o[db] = zero16();
-        m = -INFINITY;
-        l = 0.f;
-        for (int k = a.has_pre ? 0 : 1; k < (PRE ? 1 : 2); ++k) {
-          const SeqCaches& kv = caches(k);
-          const Part pt = open(k);
-          const int64_t head = g * kv.head_stride + (kv.slot ? 0 : pt.sq * kv.seq_stride);
-          for (int u = pt.tile0 * kTok; u < min(pt.tile1 * kTok, pt.rg.cnt); ++u) {
-            const int t = pt.rg.token(u);
-            const int row = kv.slot ? (int)min((uint32_t)kv.slot[pt.sq * kv.slot_stride + t], (uint32_t)kv.pool_last) : t;
-            const int64_t at = head + row * kv.tok_stride;
-            float x = 0.f;
+      for (int db = 0; db < DB; ++db) o[w][db] = zero16();
+      m[w] = -INFINITY;
+      l[w] = 0.f;
+      for (int k = has_pre ? 0 : 1; k < (PRE ? 1 : 2); ++k) {
+        const SeqCaches& kv = k ? b.own : b.pre;
+        const Part pt = open(k);
+        const int64_t head = g * kv.head_stride + (kv.slot ? 0 : pt.sq * kv.seq_stride);
+        for (int u = pt.tile0 * kTok; u < min(pt.tile1 * kTok, pt.rg.cnt); ++u) {
+          const int t = pt.rg.token(u);
+          const int row = kv.slot ? (int)min((uint32_t)kv.slot[pt.sq * kv.slot_stride + t], (uint32_t)kv.pool_last) : t;
+          const int64_t at = head + row * kv.tok_stride;
+          float x = 0.f;
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-              const u32x4 kk = ldg_u4(kv.k + at + 16 * ks + 8 * hf2);
+          for (int ks = 0; ks < KS; ++ks) {
+            const u32x4 kk = ldg_u4(kv.k + at + 16 * ks + 8 * hf2);
 #pragma unroll
-              for (int j = 0; j < 8; ++j) x = fmaf(elem<F16>(chunk_elem(kk, j)), elem<F16>(chunk_elem(qf[ks], j)), x);
-            }
-            x = sum32(x) * a.sl2;
-            if (!(t < pt.row_hi && (t >= pt.row_lo || t < pt.rg.n_first))) continue;
-            const float nm = fmaxf(m, x), ref = nm == -INFINITY ? 0.f : nm;
-            const float al = __builtin_amdgcn_exp2f(m - ref), w = __builtin_amdgcn_exp2f(x - ref);
-            m = nm;
-            l = l * al + w;
-#pragma unroll
-            for (int db = 0; db < DB; ++db)
-#pragma unroll
-              for (int r = 0; r < 16; ++r)
-                o[db][r] = fmaf(w, elem<F16>(kv.v[at + 32 * db + 8 * (r / 4) + 4 * hf2 + r % 4]), o[db][r] * al);
+            for (int j = 0; j < 8; ++j) x = fmaf(elem<F16>(chunk_elem(kk, j)), elem<F16>(chunk_elem(qf[w][ks], j)), x);
           }
+          x = sum32(x) * b.sl2;
+          if (!(t < pt.row_hi[w] && (t >= pt.row_lo[w] || t < pt.rg.n_first))) continue;
+          const float nm = fmaxf(m[w], x), ref = nm == -INFINITY ? 0.f : nm;
+          const float al = __builtin_amdgcn_exp2f(m[w] - ref), p = __builtin_amdgcn_exp2f(x - ref);
+          m[w] = nm;
+          l[w] = l[w] * al + p;
+#pragma unroll
+          for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+              o[w][db][r] = fmaf(p, elem<F16>(kv.v[at + 32 * db + 8 * (r / 4) + 4 * hf2 + r % 4]), o[w][db][r] * al);
         }
       }
     }
 
-    if (PRE || x0 > 0 || x1 < work) {
+    if (PRE || begun || !ends) {
       // partial sums: an opening share continues a block that another began
-      const bool goes_on = !PRE && opening && x0 > 0;
+      const bool goes_on = !PRE && first && begun;
       const int64_t item = PRE ? (int64_t)blockIdx.x : 2 * (int64_t)blockIdx.x + (goes_on ? 0 : 1);
-      if (goes_on) record.w = x1 < work ? 1 : 2;
-      else record = make_int4(s, rb, 1, record.w);
-      if (row < n_rows) {
+      if (goes_on) record.w = ends ? 2 : 1;
+      else record = make_int4(s2, rb2, 1, record.w);
+#pragma unroll
+      for (int w = 0; w < kRW; ++w) {
+        const int row = (wave * kRW + w) * 32 + c2;
+        if (row >= rows2) continue;
         const int64_t at = item * kRB + row;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
           for (int r = 0; r < 16; r += 4)
-            *reinterpret_cast<f32x4*>(sp.o + at * D + 32 * db + 2 * r + 4 * hf2) = f32x4{o[db][r], o[db][r + 1], o[db][r + 2], o[db][r + 3]};
-        if (hf2 == 0) *reinterpret_cast<float2*>(sp.ml + at * 2) = make_float2(m, l);
+            *reinterpret_cast<f32x4*>(sp.o + at * D + 32 * db + 2 * r + 4 * hf2) =
+                f32x4{o[w][db][r], o[w][db][r + 1], o[w][db][r + 2], o[w][db][r + 3]};
+        if (hf2 == 0) *reinterpret_cast<float2*>(sp.ml + at * 2) = make_float2(m[w], l[w]);
       }
       continue;
     }
-    // A wave's rows go through LDS (its own tenth of the tiles), so that a store
+    // A wave's rows go through LDS (its own part of the tiles), so that a store
     // covers whole rows.
     constexpr int kPitch = 2 * D + 16;
-    static_assert(kNW * 32 * kPitch <= 6 * L::kTileB);
+    static_assert(kRB * kPitch <= 6 * L::kTileB);
     tile_barrier();                                  // no wave reads tiles any more
-    char* mine = tiles + wave * 32 * kPitch;
-    if (wave_on) {
-      const float inv = l == 0.f ? 0.f : 1.f / l;
-      const float lse = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
-      bool bad = l != 0.f && !__builtin_isfinite(lse);
+#pragma unroll
+    for (int w = 0; w < kRW; ++w) {
+      const int row0 = (wave * kRW + w) * 32, row = row0 + c2;
+      if (row0 >= rows2) continue;
+      char* mine = tiles + row0 * kPitch;
+      const float inv = l[w] == 0.f ? 0.f : 1.f / l[w];
+      const float lse = l[w] == 0.f ? -INFINITY : (m[w] + __builtin_amdgcn_logf(l[w])) * kLn2;
+      bool bad = l[w] != 0.f && !__builtin_isfinite(lse);
 #pragma unroll
       for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -686,25 +808,25 @@ __global__ __launch_bounds__(kNT) void attend_wide_kernel(AttendArgs a, SplitSpa
           float y[4];
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            y[j] = l == 0.f ? 0.f : o[db][r + j] * inv;
+            y[j] = l[w] == 0.f ? 0.f : o[w][db][r + j] * inv;
             bad |= !__builtin_isfinite(y[j]);
           }
           *reinterpret_cast<uint2*>(mine + c2 * kPitch + (32 * db + 2 * r + 4 * hf2) * 2) =
               make_uint2(pack2<F16>(y[0], y[1]), pack2<F16>(y[2], y[3]));
         }
-      if (bad && row < n_rows) latch_nonfinite(a.nonfinite);
-      if (a.lse && hf2 == 0 && row < n_rows) {
-        const int q = rb * kRB + row;
-        a.lse[(int64_t)(r0 + q / a.group) * a.Hq + g * a.group + q % a.group] = lse;
+      if (bad && row < rows2) latch_nonfinite(b.nonfinite);
+      if (b.lse && hf2 == 0 && row < rows2) {
+        const int q = rb2 * kRB + row;
+        b.lse[(int64_t)(r2 + q / b.group) * b.Hq + g * b.group + q % b.group] = lse;
       }
       wait_lds_reads();                              // the wave's own writes, too
 #pragma unroll
       for (int j = 0; j < 32 / L::LANES; ++j) {
-        const int r = j * L::LANES + ln / L::CH, ch2 = ln % L::CH, gr = wave * 32 + r;
-        if (gr < n_rows) {
-          const int q = rb * kRB + gr;
-          const int64_t out = (int64_t)(r0 + q / a.group) * a.Hq + g * a.group + q % a.group;
-          *reinterpret_cast<u32x4*>(a.o + out * D + ch2 * 8) = *reinterpret_cast<const u32x4*>(mine + r * kPitch + ch2 * 16);
+        const int r = j * L::LANES + ln / L::CH, ch2 = ln % L::CH, gr = row0 + r;
+        if (gr < rows2) {
+          const int q = rb2 * kRB + gr;
+          const int64_t out = (int64_t)(r2 + q / b.group) * b.Hq + g * b.group + q % b.group;
+          *reinterpret_cast<u32x4*>(b.o + out * D + ch2 * 8) = *reinterpret_cast<const u32x4*>(mine + r * kPitch + ch2 * 16);
         }
       }
     }
