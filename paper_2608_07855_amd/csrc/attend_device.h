@@ -237,8 +237,8 @@ __device__ __forceinline__ Range seen_range(const SeqCaches& c, int sq, int n, i
       k.take(d);
     }
     hi = last ? n : h.lo;
-    lo = w.lo;
-    ns = k.lo;
+    lo = window ? w.lo : 0;
+    ns = window ? k.lo : 0;
   } else {
     auto in = [&](long long t) { return (int)min(max(t, 0ll), (long long)n); };
     hi = in((long long)qmax + 1 - base);

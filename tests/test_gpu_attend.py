@@ -73,6 +73,38 @@ def test_gapped_positions(ckv, paged, window, n_sink):
     _run(ckv, b, window, n_sink, what="gaps")
 
 
+@pytest.mark.parametrize("rows", [1, 3])
+@pytest.mark.parametrize("window,n_sink", [(0, 0), (0, 4), (50, 0), (50, 11), (1, 0), (5000, 3)])
+def test_gapped_single_tokens(ckv, rows, window, n_sink):
+    """The same, few rows each, with caches that are split among others."""
+    b = Batch(51, [200, 3, 90, 513, 9000], [rows] * 5, 8, 2, 128, gaps=True)
+    _run(ckv, b, window, n_sink, what="gaps")
+
+
+@pytest.mark.parametrize("seed", range(48))
+def test_any_batch(ckv, seed):
+    """Batches drawn over everything a view may hold."""
+    rng = np.random.default_rng(seed)
+    n = int(rng.choice([1, 2, 5, 70]))
+    long = int(rng.choice([40, 300, 2500])) if n < 70 else 30
+    lens = rng.integers(0, long + 1, n)
+    few = rng.random() < 0.5
+    rows = rng.integers(0, 3 if few else 90, n) if n < 70 else rng.integers(0, 4, n)
+    hq, hkv, d = [(4, 1, 64), (6, 6, 64), (8, 2, 128), (20, 4, 64), (17, 1, 128)][int(rng.integers(5))]
+    gaps, given = rng.random() < 0.5, rng.random() < 0.3
+    prefix = int(rng.choice([0, 0, 1, 130, 700]))
+    qpos = None
+    if given:
+        qpos = [rng.integers(-3, 3 * (prefix + long) + 3, r) for r in rows]
+    elif not gaps or prefix:
+        lens = np.maximum(lens, rows) if rng.random() < 0.7 else lens
+    b = Batch(1000 + seed, lens, rows, hq, hkv, d, "fp16" if rng.random() < 0.5 else "bf16", rng.random() < 0.6, gaps, qpos,
+              prefix, gaps, lead=int(rng.integers(3)), tail=int(rng.integers(3)))
+    window = 0 if prefix else int(rng.choice([0, 1, 30, 64, 500, 1 << 30]))
+    n_sink = 0 if prefix else int(rng.choice([0, 1, 40, 1 << 30]))
+    _run(ckv, b, window, n_sink, max_rows=int(rng.choice([1, max(1, int(rows.max(initial=1))), 500])), what=f"seed {seed}")
+
+
 @pytest.mark.parametrize("window", [0, 8])
 def test_given_positions(ckv, window):
     """Rows at positions of their own, out of order and far apart, some before every token, one at the far end."""
