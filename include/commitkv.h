@@ -568,7 +568,8 @@ typedef struct ckv_batch_view {
  * a sequence may own none).  qpos[r] is the row's absolute position; NULL:
  * the rows of a sequence are its last tokens, one each (row j of R is token
  * n_tokens - R + j; a row before token 0 of a cache with positions sees
- * nothing).  Query head h reads KV head h / (n_q_heads / n_kv_heads).
+ * nothing).  With another order of cu_rows the call stays in bounds, and the
+ * outputs are undefined.  Query head h reads KV head h / (n_q_heads / n_kv_heads).
  * max_rows is the host's estimate of the most rows a sequence owns; it picks
  * the kernels (1: single tokens), and any count is served right. */
 typedef struct ckv_query_view {
@@ -599,20 +600,27 @@ typedef struct ckv_query_view {
  * Values, keys and slots of tokens that no row of a sequence sees do not
  * reach its outputs, whatever they hold.
  * Precision: float32 logits, maxima, sums and accumulation; softmax weights
- * rounded to the batch's type before they multiply the values.
+ * rounded to the batch's type before they multiply the values (up to 32 rows a
+ * sequence and KV head: to two values of the type, weight and rest).
  *
  * The call reads counts and lengths on the device only, so a captured step
  * replays with grown caches.  Partial sums live in a workspace of the context
  * that later calls share: calls and replays of one context that overlap in
  * time need contexts of their own.  Memory a captured graph refers to is kept
- * until ckv_destroy, and an equal call made before the capture (the same
- * n_seq, n_rows, max_rows, heads) leaves the workspace it needs.
+ * until ckv_destroy (it counts toward ckv_workspace_bytes and the limit of
+ * ckv_set_workspace_limit), and an equal call made before the capture (the same
+ * n_seq, n_rows, max_rows, max_tokens, heads) leaves the workspace it needs.
  * Under a workspace limit that leaves no room for partial sums the call runs
  * without splitting sequences (more slowly, the same results up to rounding).
  *
  * Errors: CKV_ERR_ARG for NULL pointers, misaligned rows, an unknown type, a
- * negative window or n_sink, outputs that overlap the queries; CKV_ERR_SHAPE
- * for head counts, widths and strides.
+ * negative window or n_sink, outputs that overlap the queries or each other
+ * (that they lie outside the caches is the caller's to see to); CKV_ERR_SHAPE
+ * for head counts, widths and strides; CKV_ERR_UNSUPPORTED for more than about
+ * 2^23 row blocks and KV heads together; CKV_ERR_NOMEM, also inside a capture
+ * whose equal call was not made before; CKV_ERR_NONFINITE by a later call, as
+ * everywhere, where a row sees a key or value that makes its output infinite
+ * or NaN.
  */
 int ckv_attend_window(ckv_ctx* ctx, const ckv_batch_view* kv,
                       const ckv_query_view* q, int32_t window, int32_t n_sink,
@@ -694,7 +702,8 @@ typedef struct ckv_slot_step {
  * into it wherever a row is formed.
  * Errors: CKV_ERR_ARG (NULL pointers, block_size or sizes out of range,
  * block_table missing where block_size > 1, outputs that overlap inputs or
- * each other).
+ * each other: a table counts from its first to its last row, so tables whose
+ * rows alternate in one buffer overlap).
  */
 int ckv_build_slots(ckv_ctx* ctx, const ckv_slot_step* step);
 

@@ -41,8 +41,11 @@ constexpr int kMaxSplitTokens = 8192;
 // whole of a 40-layer commit; a 65536-token layer (45 MB) fills the device by
 // itself, and 8 share a launch.
 constexpr size_t kBatchBytes = size_t(384) << 20;
-// arrival counts of the attention calls, one int for every split
-constexpr size_t kAttendCounts = size_t(1) << 18;
+// Arrival counts of the attention calls, an int an item: only calls of less
+// than 4096 row blocks are split, into 1024 items more and one a KV head.
+constexpr size_t kAttendCounts = size_t(1) << 16;
+// workgroups of up to 512 threads in a launch (a grid has less than 2^32 threads)
+constexpr int64_t kMostGroups = (int64_t(1) << 23) - 1;
 // the token-mass kernel (126 registers, 40 KB of LDS) keeps two workgroups per
 // compute unit busy: 512 token chunks measured 31.7 us against 35.3 us with 256
 constexpr int kMassBlocks = 512;
@@ -225,16 +228,20 @@ bool allocate(ckv_ctx::Arena& a, size_t bytes) {
   return true;
 }
 
+// what the attention calls hold: captured graphs may refer to it, so nothing frees it
+size_t attend_held(const ckv_ctx* c) { return c->attend_ws.cap + c->outgrown_bytes; }
+
 int ensure_ws(ckv_ctx* c, size_t need) {
   if (need <= c->ws.cap) return CKV_OK;
-  if (c->ws_limit && need > c->ws_limit)
-    return fail(c, CKV_ERR_NOMEM, "workspace of %zu bytes exceeds the limit of %zu", need, c->ws_limit);
-  size_t want = std::max(need, c->ws.cap + c->ws.cap / 2);
-  if (c->ws_limit) want = std::min(want, c->ws_limit);
+  const size_t most = c->ws_limit ? c->ws_limit - std::min(c->ws_limit, attend_held(c)) : SIZE_MAX;
+  if (need > most)
+    return fail(c, CKV_ERR_NOMEM, "workspace of %zu bytes exceeds the limit of %zu (%zu held for attention)", need, c->ws_limit,
+                attend_held(c));
+  const size_t want = std::min(most, std::max(need, c->ws.cap + c->ws.cap / 2));
   CKV_HIP(c, hipStreamSynchronize(c->stream));   // in-flight work may still use the old arena
   release(c->ws);
   // a single call goes before a batch's memory, at the limit and on a full device
-  if (c->ws_limit && c->batch_ws.cap > c->ws_limit - want) release(c->batch_ws);
+  if (c->batch_ws.cap > most - want) release(c->batch_ws);
   if (allocate(c->ws, want)) return CKV_OK;
   if (c->batch_ws.p) {
     release(c->batch_ws);
@@ -246,7 +253,7 @@ int ensure_ws(ckv_ctx* c, size_t need) {
 // bytes a run of a batch may hold under the workspace limit, beside `single`
 // bytes for single calls
 size_t batch_limit(const ckv_ctx* c, size_t single) {
-  return c->ws_limit ? c->ws_limit - std::min(c->ws_limit, std::max(c->ws.cap, single)) : SIZE_MAX;
+  return c->ws_limit ? c->ws_limit - std::min(c->ws_limit, std::max(c->ws.cap, single) + attend_held(c)) : SIZE_MAX;
 }
 
 int ensure_batch_ws(ckv_ctx* c, size_t need) {
@@ -264,11 +271,11 @@ int ensure_batch_ws(ckv_ctx* c, size_t need) {
 // first kAttendCounts bytes, split partials behind them.  *room is false where
 // the workspace limit leaves none.  No stream is waited for: what is outgrown
 // stays where it is, for work under way and for captured graphs.
-int ensure_attend_ws(ckv_ctx* c, size_t counts, size_t part, bool* room) {
+int ensure_attend_ws(ckv_ctx* c, size_t part, bool* room) {
   const size_t need = kAttendCounts + part;
-  *room = counts <= kAttendCounts;
-  if (!*room || need <= c->attend_ws.cap) return CKV_OK;
-  const size_t held = c->ws.cap + c->batch_ws.cap + c->attend_ws.cap + c->outgrown_bytes;
+  *room = true;
+  if (need <= c->attend_ws.cap) return CKV_OK;
+  const size_t held = c->ws.cap + c->batch_ws.cap + attend_held(c);
   size_t want = std::max(need, 2 * c->attend_ws.cap);
   if (c->ws_limit) {
     const size_t left = c->ws_limit - std::min(c->ws_limit, held);
@@ -1828,7 +1835,7 @@ int attend(ckv_ctx* c, const ckv_batch_view* pre, const ckv_batch_view* kv, cons
   // 16, so K and V are read twice at most, the second time from L2), the rows of
   // all sequences together over the shared tokens before it.  More rows fill
   // the matrix units by themselves: they read both parts in one pass.
-  const bool few = (int64_t)q->max_rows * a.group <= 32;
+  bool few = (int64_t)q->max_rows * a.group <= 32;
   AttendPlan p = few ? plan_narrow(a, kv->max_tokens, true) : plan_wide(a, true);
   PrefixPlan pf = {0, 0, 0};
   if (pre && few) pf = plan_prefix(a);
@@ -1837,16 +1844,16 @@ int attend(ckv_ctx* c, const ckv_batch_view* pre, const ckv_batch_view* kv, cons
   const size_t pre_bytes = floats(pre_items, pf.rows);
   const size_t own_bytes = !p.split ? 0 : floats(p.items, p.rows) + (few ? 0 : p.items * sizeof(int4));
   bool room = true;
-  if (own_bytes + pre_bytes > 0) {
-    const size_t counts = few && p.split ? (size_t)p.items * sizeof(int) : 0;
-    if (int rc = ensure_attend_ws(c, counts, own_bytes + pre_bytes, &room)) return rc;
-  }
+  if (std::max(p.grid, few ? pre_items : 0) > kMostGroups)
+    return fail(c, CKV_ERR_UNSUPPORTED, "%d rows of %d sequences and %d KV heads are more than one call can launch", q->n_rows,
+                kv->n_seq, kv->n_kv_heads);
+  if (own_bytes + pre_bytes > 0)
+    if (int rc = ensure_attend_ws(c, own_bytes + pre_bytes, &room)) return rc;
   if (!room) {
-    if (pre && few) {
-      CKV_LAUNCH(c, "attend", launch_attend_rows(a, c->stream));
-      return CKV_OK;
-    }
+    // without partial sums, the many-rows kernel alone reads two parts in one pass
+    few = few && !pre;
     p = few ? plan_narrow(a, kv->max_tokens, false) : plan_wide(a, false);
+    if (p.grid > kMostGroups) return fail(c, CKV_ERR_NOMEM, "the workspace limit leaves no room for the call's partial sums");
   }
   auto space = [&](size_t off, int64_t items, int rows) {
     SplitSpace sp;

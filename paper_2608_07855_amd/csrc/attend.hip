@@ -31,80 +31,6 @@ __device__ __forceinline__ float sum_rows16(float v) {
   return sum32(__uint_as_float(r[0]) + __uint_as_float(r[1]));
 }
 
-// Without a workspace for partial sums (a workspace limit): one wave per (row,
-// query head), 64 tokens at a time, one per lane; then every lane adds their
-// weighted values into its own widths.
-template <int D, bool F16>
-__global__ __launch_bounds__(256) void attend_rows_kernel(AttendArgs a) {
-  const int lane = threadIdx.x & 63;
-  const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int r = (int)(item / a.Hq), h = (int)(item % a.Hq);
-  if (r >= a.n_rows) return;
-  const int s = row_seq(a, r);
-  if (s < 0) return;
-  const int g = h / a.group;
-  const int n = seq_tokens(a.own, s), base = a.has_pre ? seq_tokens(a.pre, 0) : 0;
-  const int r0 = row_start(a, s);
-  const int qp = row_position(a, s, r0, row_start(a, s + 1) - r0, r - r0, n, base);
-  const uint16_t* q = a.q + r * a.q_row_stride + h * a.q_head_stride;
-  constexpr int PW = D / 64;
-  float m = -INFINITY, l = 0.f, acc[PW] = {};
-  for (int part = a.has_pre ? 0 : 1; part < 2; ++part) {
-    const SeqCaches& c = part ? a.own : a.pre;
-    const int sq = part ? s : 0, nt = part ? n : base, b = part ? base : 0;
-    const int64_t head = g * c.head_stride + (c.slot ? 0 : sq * c.seq_stride);
-    for (int t0 = 0; t0 < nt; t0 += 64) {
-      const int t = t0 + lane;
-      bool vis = t < nt;
-      int64_t at = 0;
-      float x = -INFINITY;
-      if (vis) vis = sees(c.pos ? c.pos[sq * c.pos_stride + t] : b + t, qp, a.window, a.n_sink);
-      if (vis) {
-        const int row = c.slot ? (int)min((uint32_t)c.slot[sq * c.slot_stride + t], (uint32_t)c.pool_last) : t;
-        at = head + row * c.tok_stride;
-        x = 0.f;
-        for (int e = 0; e < D; e += 8) {
-          const u32x4 kk = ldg_u4(c.k + at + e), qq = ldg_u4(q + e);
-          for (int j = 0; j < 8; ++j) x = fmaf(elem<F16>(chunk_elem(kk, j)), elem<F16>(chunk_elem(qq, j)), x);
-        }
-        x *= a.sl2;
-      }
-      unsigned long long todo = __ballot(vis);
-      if (!todo) continue;
-      float mx = x;
-      for (int off = 32; off; off >>= 1) mx = fmaxf(mx, __shfl_xor(mx, off, 64));
-      mx = fmaxf(mx, m);
-      const float ref = mx == -INFINITY ? 0.f : mx;
-      const float al = exp2f(m - ref);
-      const float p = vis ? exp2f(x - ref) : 0.f;
-      m = mx;
-      float sum = p;
-      for (int off = 32; off; off >>= 1) sum += __shfl_xor(sum, off, 64);
-      l = l * al + sum;
-      for (int w = 0; w < PW; ++w) acc[w] *= al;
-      while (todo) {
-        const int j = __ffsll((long long)todo) - 1;
-        todo &= todo - 1;
-        const float pj = __shfl(p, j, 64);
-        const int64_t aj = __shfl((long long)at, j, 64);
-        for (int w = 0; w < PW; ++w) acc[w] = fmaf(pj, elem<F16>(c.v[aj + w * 64 + lane]), acc[w]);
-      }
-    }
-  }
-  const int64_t out = (int64_t)r * a.Hq + h;
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  bool bad = false;
-  for (int w = 0; w < PW; ++w) {
-    const float y = l == 0.f ? 0.f : acc[w] * inv;
-    bad |= !__builtin_isfinite(y);
-    a.o[out * D + w * 64 + lane] = to_elem<F16>(y);
-  }
-  const float lse = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
-  bad |= l != 0.f && !__builtin_isfinite(lse);
-  if (a.lse && lane == 0) a.lse[out] = lse;
-  if (bad) latch_nonfinite(a.nonfinite);
-}
-
 // ---------------------------------------------------------------------------
 // Few rows: a wave takes 16 query rows and its own tokens, 32 at a time.
 //
@@ -155,7 +81,9 @@ __global__ __launch_bounds__(64 * NW) void attend_narrow_kernel(AttendArgs a, Sp
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, q = lane >> 4;
   const int g = blockIdx.x % a.Hkv;
   const Item it = find_item<NT, L::kRows>(a, blockIdx.x / a.Hkv, target, min_chunk, ish);
-  if (it.s < 0) return;
+  // (a block whose splits pass the grid, which rows out of order can make, is left
+  // by all of them: none counts an arrival that the others do not)
+  if (it.s < 0 || (it.e - it.split + it.n_split) * a.Hkv > gridDim.x) return;
   const int s = it.s, n = seq_tokens(a.own, s), base = a.has_pre ? seq_tokens(a.pre, 0) : 0;
   const int r0 = row_start(a, s), R = row_start(a, s + 1) - r0;
   const int n_rows = min(L::kRows, R * a.group - it.rb * L::kRows);      // rows of this block
@@ -394,7 +322,10 @@ __global__ __launch_bounds__(64 * NW) void attend_narrow_kernel(AttendArgs a, Sp
   __syncthreads();
   auto finish = [&](int row, int w4, Joined j) {
     const int rr = it.rb * L::kRows + row;
-    if (pp.n_split) add_prefix(a, pp, D, (r0 - row_start(a, 0)) * a.group + rr, g, w4, j);
+    if (pp.n_split) {
+      const int first = row_start(a, 0), row = r0 + rr / a.group;     // (rows out of order may lie outside the prefix's)
+      if (row >= first && row < row_start(a, a.own.n_seq)) add_prefix(a, pp, D, (r0 - first) * a.group + rr, g, w4, j);
+    }
     store_row<D, F16>(a, r0, rr, g, w4, j.acc, j.m, j.l);
   };
   constexpr int TPR = D / 4;                 // threads of a row, four widths each
@@ -453,19 +384,6 @@ __global__ __launch_bounds__(64 * NW) void attend_narrow_kernel(AttendArgs a, Sp
 
 }  // namespace
 
-hipError_t launch_attend_rows(const AttendArgs& a, hipStream_t s) {
-  const int64_t items = (int64_t)a.n_rows * a.Hq;
-  const dim3 grid((unsigned)((items + 3) / 4));
-  if (a.D == 64) {
-    if (a.f16) attend_rows_kernel<64, true><<<grid, 256, 0, s>>>(a);
-    else attend_rows_kernel<64, false><<<grid, 256, 0, s>>>(a);
-  } else {
-    if (a.f16) attend_rows_kernel<128, true><<<grid, 256, 0, s>>>(a);
-    else attend_rows_kernel<128, false><<<grid, 256, 0, s>>>(a);
-  }
-  return hipGetLastError();
-}
-
 AttendPlan plan_narrow(const AttendArgs& a, int64_t max_tokens, bool room) {
   AttendPlan p;
   p.rows = 16;
@@ -484,14 +402,14 @@ AttendPlan plan_narrow(const AttendArgs& a, int64_t max_tokens, bool room) {
     p.min_chunk = INT_MAX;                                              // no splits
     e = blocks;
   }
-  p.items = e * a.Hkv;
+  p.items = p.grid = e * a.Hkv;
   p.split = p.min_chunk != INT_MAX;
   return p;
 }
 
 hipError_t launch_attend_narrow(const AttendArgs& a, const AttendPlan& p, const SplitSpace& sp, const PrefixParts& pp,
                                 hipStream_t s) {
-  const dim3 grid((unsigned)p.items);
+  const dim3 grid((unsigned)p.grid);
   const bool tab = a.own.slot || a.own.pos;
 #define CKV_NARROW(D, F16, TAB) \
   if (p.alone) attend_narrow_kernel<D, F16, TAB, 512 / D><<<grid, 64 * 512 / D, 0, s>>>(a, sp, p.target, p.min_chunk, pp); \

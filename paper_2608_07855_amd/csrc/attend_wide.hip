@@ -868,7 +868,8 @@ AttendPlan plan_wide(const AttendArgs& a, bool room) {
   p.alone = false;
   p.min_chunk = 0;
   p.target = std::max(1, 256 / a.Hkv);             // a workgroup a compute unit
-  p.blocks = (int64_t)a.n_rows * a.group / kRB + std::min(a.own.n_seq, a.n_rows);   // of a head, at most
+  const int64_t blocks = (int64_t)a.n_rows * a.group / kRB + std::min(a.own.n_seq, a.n_rows);   // of a head, at most
+  p.grid = std::max<int64_t>(p.target, blocks) * a.Hkv;
   p.items = 2 * (int64_t)p.target * a.Hkv;
   p.split = room && p.target > 1;
   return p;
@@ -908,7 +909,7 @@ PrefixPlan plan_prefix(const AttendArgs& a) {
   }
 
 hipError_t launch_attend_wide(const AttendArgs& a, const AttendPlan& p, const SplitSpace& sp, hipStream_t s) {
-  const dim3 grid((unsigned)(std::max<int64_t>(p.target, p.blocks) * a.Hkv));
+  const dim3 grid((unsigned)p.grid);
   const bool tab = a.own.slot || (a.has_pre && a.pre.slot);
   CKV_WIDE2(false, grid, p.target, p.split ? 0 : 1)
   return hipGetLastError();

@@ -403,7 +403,6 @@ struct AttendArgs {
   float* lse;             // [n_rows][Hq], or null
   uint32_t* nonfinite;
 };
-hipError_t launch_attend_rows(const AttendArgs& a, hipStream_t s);
 
 // Split partials: item by item, a row block's rows each.
 struct SplitSpace {
@@ -425,10 +424,11 @@ struct PrefixParts {
 // partial sums.  split: whether there are.  Many rows: `target` equal shares a
 // KV head, at most two partial row blocks each.
 struct AttendPlan {
-  int64_t items, blocks;
-  int rows, target, min_chunk;
+  int64_t items, grid;   // items with partial sums; workgroups
+  int rows, target;
   bool split;
-  bool alone;      // few-rows kernel: workgroups that take a compute unit each
+  int min_chunk;   // few rows: tokens of a split at least
+  bool alone;      // few rows: workgroups that take a compute unit each
 };
 AttendPlan plan_narrow(const AttendArgs& a, int64_t max_tokens, bool room);
 AttendPlan plan_wide(const AttendArgs& a, bool room);

@@ -430,7 +430,63 @@ def test_workspace_limit(ckv):
     ctx.close()
 
 
+def test_workspace_limit_counts_partial_sums(ckv):
+    """What the attention holds counts for the calls that come after it, single ones and batches."""
+    from tests.test_gpu_batch import WANT, _problem
+    P, _ = ckv
+    one = _problem(P, 16, 8, 64, 4096, 8, 16, False, seed=3)
+    ctx = P.Context(0)
+    b = Batch(46, [9000, 100], [1, 1], 8, 2, 128)
+    b.run(P, ctx, b.device(P))
+    held = ctx.workspace_bytes()
+    assert held > 0
+    ctx.set_workspace_limit(held + 4096)
+    with pytest.raises(P.CKVError) as e:
+        P.ckv_measure_page_effects(ctx, *one[:3], want=WANT)
+    assert e.value.code == -5
+    ctx.set_workspace_limit(held + (64 << 20))
+    got = P.ckv_measure_page_effects_batch(ctx, *[[one[j]] * 3 for j in range(3)], want=WANT)
+    assert len(got) == 3 and ctx.workspace_bytes() <= held + (64 << 20)
+    ctx.close()
+
+
+@pytest.mark.parametrize("prefix", [0, 300])
+def test_rows_out_of_order(ckv, prefix):
+    """cu_rows that do not ascend: any outputs, no row past n_rows, and the next call is right again."""
+    P, ctx = ckv
+    b = Batch(47, [5000, 4000, 6000, 3000], [1, 1, 1, 1], 8, 2, 128, prefix=prefix, lead=1, tail=1)
+    v = b.device(P)
+    for cu in ([5, 0, 3, 1, 4], [0, 6, 0, 6, 0], [-9, 100, -9, 100, 2], [6, 6, 0, 0, 6]):
+        for most in (1, 200):
+            w = P.query_view(v["q"]._keep[0], torch.tensor(cu, dtype=torch.int32, device="cuda"), max_rows=most)
+            o = torch.zeros((8, 8, 128), dtype=torch.bfloat16, device="cuda")
+            lse = torch.zeros((8, 8), device="cuda")
+            if prefix:
+                P.ckv_attend_shared(ctx, v["prefix"], v["kv"], w, o=o[:6], lse=lse[:6])
+            else:
+                P.ckv_attend_window(ctx, v["kv"], w, o=o[:6], lse=lse[:6])
+            torch.cuda.synchronize()
+            assert not o[6:].any() and not lse[6:].any()
+            check(b, b.run(P, ctx, v), b.want(), f"after {cu}")
+
+
 # ------------------------------------------------------------------- refusals
+
+def test_more_than_a_launch_holds(ckv):
+    """2^20 sequences of 32 KV heads, none with a row: more row blocks than a grid has."""
+    P, ctx = ckv
+    n = 1 << 20
+    k = torch.zeros((32, 4, 64), dtype=torch.bfloat16, device="cuda")
+    zero = torch.zeros(n + 1, dtype=torch.int32, device="cuda")
+    kv = P.batch_view(k, k.clone(), zero[:n], slot=torch.zeros((n, 1), dtype=torch.int32, device="cuda"))
+    q = torch.zeros((n, 32, 64), dtype=torch.bfloat16, device="cuda")
+    o = torch.zeros_like(q)
+    for most in (1, 1000):
+        with pytest.raises(P.CKVError) as e:
+            P.ckv_attend_window(ctx, kv, P.query_view(q, zero, max_rows=most), o=o)
+        assert e.value.code == -4
+
+
 
 def test_refusals(ckv):
     P, ctx = ckv
