@@ -36,8 +36,7 @@ namespace {
 // ---------------------------------------------------------------------------
 constexpr float kLag = 8.f;   // log2 units
 constexpr int kAhead = 4;     // operands read from LDS ahead of their products
-constexpr int kRW = 1;        // 32-row blocks of a wave
-constexpr int kNW = 8 / kRW, kNT = 64 * kNW, kRB = 256, kTok = 64;
+constexpr int kNW = 8, kNT = 64 * kNW, kRB = 256, kTok = 64;
 
 template <int D>
 struct Wide {
@@ -225,7 +224,7 @@ struct Part {
   Range rg;
   int n, base, sq, tile0, tile1;
   int full_lo, full_hi;   // tokens that every row of the wave sees: [full_lo, full_hi), and first ones before full_hi
-  int row_lo[kRW], row_hi[kRW];   // tokens that the lane's rows see: [row_lo, row_hi), and first ones before row_hi
+  int row_lo, row_hi;   // tokens that the lane's row sees: [row_lo, row_hi), and first ones before row_hi
 };
 
 // The kernel's first argument, read from memory where it is used next.
@@ -243,7 +242,7 @@ enum Kept { kS, kRb, kR0, kRows, kX0, kX1 = kX0 + 2, kWork = kX1 + 2, kQmin = kW
 // partial sums.  Otherwise a share of the blocks (W shares a KV head), in each
 // the shared tokens first; n_split 1: whole blocks only.
 template <int D, bool F16, bool TAB, bool PRE>
-__global__ __launch_bounds__(kNT, 2 / kRW) void attend_wide_kernel(AttendArgs args, SplitSpace sp, int W, int n_split) {
+__global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, SplitSpace sp, int W, int n_split) {
   using L = Wide<D>;
   constexpr int KS = D / 16, DB = D / 32;
   __shared__ __align__(256) char tiles[L::kLds];
@@ -326,26 +325,22 @@ __global__ __launch_bounds__(kNT, 2 / kRW) void attend_wide_kernel(AttendArgs ar
       me.left = 0;
     }
 
-    // the lane's rows: their positions and queries
-    int qp[kRW], qmin = INT_MAX, qmax = INT_MIN;
-    u32x4 qf[kRW][KS];
-    const bool wave_on = wave * 32 * kRW < n_rows;
-#pragma unroll
-    for (int w = 0; w < kRW; ++w) {
-      const int i = min((wave * kRW + w) * 32 + c, n_rows - 1);
-      const int rr = rb * kRB + i, p = rr / a.group, h = g * a.group + rr % a.group;
-      if constexpr (PRE) {
-        const int row = r0 + p, rs = max(row_seq(a, row), 0), f = row_start(a, rs);
-        qp[w] = row_position(a, rs, f, row_start(a, rs + 1) - f, row - f, seq_tokens(a.own, rs), pre_n);
-      } else {
-        qp[w] = row_position(a, s, r0, R, p, seq_tokens(a.own, s), pre_n);
-      }
-      const uint16_t* qr = a.q + (int64_t)(r0 + p) * a.q_row_stride + (int64_t)h * a.q_head_stride;
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) qf[w][ks] = ldg_u4(qr + 16 * ks + 8 * hf);
-      qmin = min(qmin, qp[w]);
-      qmax = max(qmax, qp[w]);
+    // the lane's row: its position and query
+    int qp;
+    u32x4 qf[KS];
+    const bool wave_on = wave * 32 < n_rows;
+    const int i = min(wave * 32 + c, n_rows - 1);
+    const int rr = rb * kRB + i, p = rr / a.group, h = g * a.group + rr % a.group;
+    if constexpr (PRE) {
+      const int row = r0 + p, rs = max(row_seq(a, row), 0), f = row_start(a, rs);
+      qp = row_position(a, rs, f, row_start(a, rs + 1) - f, row - f, seq_tokens(a.own, rs), pre_n);
+    } else {
+      qp = row_position(a, s, r0, R, p, seq_tokens(a.own, s), pre_n);
     }
+    const uint16_t* qr = a.q + (int64_t)(r0 + p) * a.q_row_stride + (int64_t)h * a.q_head_stride;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = ldg_u4(qr + 16 * ks + 8 * hf);
+    int qmin = qp, qmax = qp;
 #pragma unroll
     for (int off = 16; off; off >>= 1) {
       qmin = min(qmin, __shfl_xor(qmin, off, 64));
@@ -383,15 +378,10 @@ __global__ __launch_bounds__(kNT, 2 / kRW) void attend_wide_kernel(AttendArgs ar
     keep(kRecord + 2, record.z);
     keep(kRecord + 3, record.w);
 
-    f32x16 o[kRW][DB];
-    float m[kRW], l[kRW];
+    f32x16 o[DB];
+    float m = -INFINITY, l = 0.f;
 #pragma unroll
-    for (int w = 0; w < kRW; ++w) {
-      m[w] = -INFINITY;
-      l[w] = 0.f;
-#pragma unroll
-      for (int db = 0; db < DB; ++db) o[w][db] = zero16();
-    }
+    for (int db = 0; db < DB; ++db) o[db] = zero16();
     bool hidden = false;          // some tile held tokens that not all rows see
 
     auto open = [&](int k) {
@@ -423,18 +413,12 @@ __global__ __launch_bounds__(kNT, 2 / kRW) void attend_wide_kernel(AttendArgs ar
           }
           return lo;
         };
-#pragma unroll
-        for (int w = 0; w < kRW; ++w) {
-          t.row_hi[w] = find(t.full_hi, t.rg.hi, qp[w]);
-          t.row_lo[w] = a.window ? find(t.rg.lo, t.rg.hi, (long long)qp[w] - a.window) : 0;
-        }
+        t.row_hi = find(t.full_hi, t.rg.hi, qp);
+        t.row_lo = a.window ? find(t.rg.lo, t.rg.hi, (long long)qp - a.window) : 0;
       } else {
         auto in = [&](long long x) { return (int)min(max(x, 0ll), (long long)t.n); };
-#pragma unroll
-        for (int w = 0; w < kRW; ++w) {
-          t.row_hi[w] = in((long long)qp[w] + 1 - t.base);
-          t.row_lo[w] = a.window ? in((long long)qp[w] - a.window + 1 - t.base) : 0;
-        }
+        t.row_hi = in((long long)qp + 1 - t.base);
+        t.row_lo = a.window ? in((long long)qp - a.window + 1 - t.base) : 0;
       }
       const int n_tiles = (t.rg.cnt + kTok - 1) / kTok;
       if constexpr (PRE) {
@@ -505,46 +489,39 @@ __global__ __launch_bounds__(kNT, 2 / kRW) void attend_wide_kernel(AttendArgs ar
       };
 
       // scores of a tile (raw products)
-      auto score = [&](int tile, f32x16 (&x)[kRW][2]) {
+      auto score = [&](int tile, f32x16 (&x)[2]) {
         const uint32_t off = (tile % 3) * L::kTileB;
 #pragma unroll
         for (int tb = 0; tb < 2; ++tb) {
-#pragma unroll
-          for (int w = 0; w < kRW; ++w) x[w][tb] = zero16();
+          x[tb] = zero16();
 #pragma unroll
           for (int ks = 0; ks < KS; ++ks) {
             const u32x4 kf = lds_read16((ka + off) ^ (32 * ks), tb * 32 * L::kRowB);
-#pragma unroll
-            for (int w = 0; w < kRW; ++w) x[w][tb] = mfma32<F16>(kf, qf[w][ks], x[w][tb]);
+            x[tb] = mfma32<F16>(kf, qf[ks], x[tb]);
           }
         }
       };
       // hides what a row does not see
-      auto mask = [&](int tile, f32x16 (&x)[kRW][2]) {
+      auto mask = [&](int tile, f32x16 (&x)[2]) {
         const int u0 = tile * kTok, u1 = u0 + kTok - 1, ta = rg.token(u0), te = rg.token(u1);
         if (te < pt.full_hi && (ta >= pt.full_lo || te < rg.n_first)) return;
         hidden = true;
         if (ta >= rg.n_first && u0 >= rg.ns) {
-#pragma unroll
-          for (int w = 0; w < kRW; ++w) {
-            const uint32_t len = max(pt.row_hi[w] - pt.row_lo[w], 0), d = ta + 4 * hf - pt.row_lo[w];
-#pragma unroll
-            for (int tb = 0; tb < 2; ++tb)
-#pragma unroll
-              for (int r = 0; r < 16; ++r)
-                x[w][tb][r] = d + (uint32_t)(32 * tb + 8 * (r / 4) + r % 4) < len ? x[w][tb][r] : -INFINITY;
-          }
-          return;
-        }
-#pragma unroll
-        for (int w = 0; w < kRW; ++w)
+          const uint32_t len = max(pt.row_hi - pt.row_lo, 0), d = ta + 4 * hf - pt.row_lo;
 #pragma unroll
           for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              const int t = rg.token(u0 + 32 * tb + 8 * (r / 4) + 4 * hf + r % 4);
-              x[w][tb][r] = t < pt.row_hi[w] && (t >= pt.row_lo[w] || t < rg.n_first) ? x[w][tb][r] : -INFINITY;
-            }
+            for (int r = 0; r < 16; ++r)
+              x[tb][r] = d + (uint32_t)(32 * tb + 8 * (r / 4) + r % 4) < len ? x[tb][r] : -INFINITY;
+          return;
+        }
+#pragma unroll
+        for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int t = rg.token(u0 + 32 * tb + 8 * (r / 4) + 4 * hf + r % 4);
+            x[tb][r] = t < pt.row_hi && (t >= pt.row_lo || t < rg.n_first) ? x[tb][r] : -INFINITY;
+          }
       };
 
       // One step: the weights of tile t from its scores x (largest one of a lane
@@ -552,22 +529,18 @@ __global__ __launch_bounds__(kNT, 2 / kRW) void attend_wide_kernel(AttendArgs ar
       // the largest of y.  A wave issues in order, so the vector work is written
       // between the products, and operands are read from LDS kAhead products
       // early; the fences keep the compiler from gathering either.
-      auto step = [&](int t, f32x16 (&x)[kRW][2], float (&mx)[kRW], f32x16 (&y)[kRW][2], float (&my)[kRW]) {
-        float ref[kRW];
+      auto step = [&](int t, f32x16 (&x)[2], float& mx, f32x16 (&y)[2], float& my) {
+        const float top = max32(mx) * sl2;
+        if (__ballot(top > m + kLag || (m == -INFINITY && top > m)) != 0ull) {
+          const float nm = top > m ? top : m;
+          const float al = nm == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - nm);
+          l *= al;
 #pragma unroll
-        for (int w = 0; w < kRW; ++w) {
-          const float top = max32(mx[w]) * sl2;
-          if (__ballot(top > m[w] + kLag || (m[w] == -INFINITY && top > m[w])) != 0ull) {
-            const float nm = top > m[w] ? top : m[w];
-            const float al = nm == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[w] - nm);
-            l[w] *= al;
-#pragma unroll
-            for (int db = 0; db < DB; ++db) o[w][db] *= al;
-            m[w] = nm;
-          }
-          ref[w] = m[w] == -INFINITY ? 0.f : m[w];
+          for (int db = 0; db < DB; ++db) o[db] *= al;
+          m = nm;
         }
-        u32x4 ph[kRW][4];
+        const float ref = m == -INFINITY ? 0.f : m;
+        u32x4 ph[4];
         {
           // past the last tile: what an older tile left, used by nobody
           const uint32_t off = ((t + 1) % 3) * L::kTileB;
@@ -578,29 +551,23 @@ __global__ __launch_bounds__(kNT, 2 / kRW) void attend_wide_kernel(AttendArgs ar
           __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
           for (int j = 0; j < 2 * KS; ++j) {
+            y[j % 2] = mfma32<F16>(kf[j % kAhead], qf[j / 2], j < 2 ? zero16() : y[j % 2]);
+            if (j + kAhead < 2 * KS) kf[j % kAhead] = read(j + kAhead);
+            // the tile's 16 pairs of scores, over the 2 KS products
 #pragma unroll
-            for (int w = 0; w < kRW; ++w) {
-              y[w][j % 2] = mfma32<F16>(kf[j % kAhead], qf[w][j / 2], j < 2 ? zero16() : y[w][j % 2]);
-              if (w == kRW - 1 && j + kAhead < 2 * KS) kf[j % kAhead] = read(j + kAhead);
-              // the tile's 16 pairs of scores, over the 2 KS products
-#pragma unroll
-              for (int q = j * 16 / (2 * KS); q < (j + 1) * 16 / (2 * KS); ++q) {
-                const int tb = q / 8, r = 2 * (q % 8);
-                const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[w][tb][r], sl2, -ref[w]));
-                const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[w][tb][r + 1], sl2, -ref[w]));
-                l[w] += p0 + p1;
-                ph[w][q / 4][q % 4] = pack2<F16>(p0, p1);
-              }
-              __builtin_amdgcn_sched_barrier(0);
+            for (int q = j * 16 / (2 * KS); q < (j + 1) * 16 / (2 * KS); ++q) {
+              const int tb = q / 8, r = 2 * (q % 8);
+              const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[tb][r], sl2, -ref));
+              const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[tb][r + 1], sl2, -ref));
+              l += p0 + p1;
+              ph[q / 4][q % 4] = pack2<F16>(p0, p1);
             }
+            __builtin_amdgcn_sched_barrier(0);
           }
           // keeps the weights here, beside the products
 #pragma unroll
-          for (int w = 0; w < kRW; ++w) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) asm volatile("" : "+v"(ph[w][j]));
-            asm volatile("" : "+v"(l[w]));
-          }
+          for (int j = 0; j < 4; ++j) asm volatile("" : "+v"(ph[j]));
+          asm volatile("" : "+v"(l));
         }
         if (t + 1 < tile1) mask(t + 1, y);
         {
@@ -613,20 +580,16 @@ __global__ __launch_bounds__(kNT, 2 / kRW) void attend_wide_kernel(AttendArgs ar
           };
 #pragma unroll
           for (int j = 0; j < kAhead; ++j) vf[j] = read(j);
-#pragma unroll
-          for (int w = 0; w < kRW; ++w) my[w] = -INFINITY;
+          my = -INFINITY;
           __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
           for (int j = 0; j < 4 * DB; ++j) {
+            o[j % DB] = mfma32<F16>(vf[j % kAhead], ph[j / DB], o[j % DB]);
+            if (j + kAhead < 4 * DB) vf[j % kAhead] = read(j + kAhead);
 #pragma unroll
-            for (int w = 0; w < kRW; ++w) {
-              o[w][j % DB] = mfma32<F16>(vf[j % kAhead], ph[w][j / DB], o[w][j % DB]);
-              if (w == kRW - 1 && j + kAhead < 4 * DB) vf[j % kAhead] = read(j + kAhead);
-#pragma unroll
-              for (int q = j * 16 / (4 * DB); q < (j + 1) * 16 / (4 * DB); ++q)
-                my[w] = max3(my[w], y[w][q / 8][2 * (q % 8)], y[w][q / 8][2 * (q % 8) + 1]);
-              __builtin_amdgcn_sched_barrier(0);
-            }
+            for (int q = j * 16 / (4 * DB); q < (j + 1) * 16 / (4 * DB); ++q)
+              my = max3(my, y[q / 8][2 * (q % 8)], y[q / 8][2 * (q % 8) + 1]);
+            __builtin_amdgcn_sched_barrier(0);
           }
         }
       };
@@ -659,15 +622,12 @@ __global__ __launch_bounds__(kNT, 2 / kRW) void attend_wide_kernel(AttendArgs ar
         // What the compiler loaded has to have arrived before the loop, or its own
         // waits inside would drain the tiles under way.
 #pragma unroll
-        for (int w = 0; w < kRW; ++w) {
-#pragma unroll
-          for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qf[w][ks]));
-          asm volatile("" : "+v"(qp[w]));
-        }
-        f32x16 xa[kRW][2], xb[kRW][2];
-        float ma[kRW], mb[kRW];
+        for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qf[ks]));
+        asm volatile("" : "+v"(qp));
+        f32x16 xa[2], xb[2];
+        float ma, mb;
         // under way, oldest first: step t, tables(t + 3), step t + 1; rows: of tile t + 2
-        auto turn = [&](int t, bool first, f32x16 (&x)[kRW][2], float (&mx)[kRW], f32x16 (&y)[kRW][2], float (&my)[kRW]) {
+        auto turn = [&](int t, bool first, f32x16 (&x)[2], float& mx, f32x16 (&y)[2], float& my) {
           if (t + 3 < tile1) wait_loads<T + KV>();
           else if (t + 2 < tile1) wait_loads<KV>();
           else if (t + 1 < tile1) wait_loads<L::LOADS>();
@@ -676,12 +636,9 @@ __global__ __launch_bounds__(kNT, 2 / kRW) void attend_wide_kernel(AttendArgs ar
           if (first && wave_on) {
             score(t, x);
             mask(t, x);
+            mx = -INFINITY;
 #pragma unroll
-            for (int w = 0; w < kRW; ++w) {
-              mx[w] = -INFINITY;
-#pragma unroll
-              for (int r = 0; r < 16; ++r) mx[w] = max3(mx[w], x[w][0][r], x[w][1][r]);
-            }
+            for (int r = 0; r < 16; ++r) mx = max3(mx, x[0][r], x[1][r]);
           }
           if (first) tile_barrier();  // K of the first tile has been read
           if (t + 2 < tile1) {
@@ -720,23 +677,20 @@ __global__ __launch_bounds__(kNT, 2 / kRW) void attend_wide_kernel(AttendArgs ar
     const bool begun = get64(kX0) > 0, ends = get64(kX1) >= get64(kWork), first = get(kOpening);
     me = {get(kNextS), get(kNextRb), get64(kNextX), get64(kLeft), false};
     record = make_int4(get(kRecord), get(kRecord + 1), get(kRecord + 2), get(kRecord + 3));
+    l = sum32(l);
+    // A token that only some rows of the block see has weight 0 in the others,
+    // and 0 times a value that is not finite is NaN: then the share's tokens
+    // are taken again one by one, each by the rows that see it.
+    bool lost = !__builtin_isfinite(l);
 #pragma unroll
-    for (int w = 0; w < kRW; ++w) {
-      l[w] = sum32(l[w]);
-      if (!hidden) continue;
-      // A token that only some rows of the block see has weight 0 in the others,
-      // and 0 times a value that is not finite is NaN: then the share's tokens
-      // are taken again one by one, each by the rows that see it.
-      bool bad = !__builtin_isfinite(l[w]);
+    for (int db = 0; db < DB; ++db)
 #pragma unroll
-      for (int db = 0; db < DB; ++db)
+      for (int r = 0; r < 16; ++r) lost |= !__builtin_isfinite(o[db][r]);
+    if (hidden && __ballot(lost) != 0ull) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) bad |= !__builtin_isfinite(o[w][db][r]);
-      if (__ballot(bad) == 0ull) continue;
-#pragma unroll
-      for (int db = 0; db < DB; ++db) o[w][db] = zero16();
-      m[w] = -INFINITY;
-      l[w] = 0.f;
+      for (int db = 0; db < DB; ++db) o[db] = zero16();
+      m = -INFINITY;
+      l = 0.f;
       for (int k = has_pre ? 0 : 1; k < (PRE ? 1 : 2); ++k) {
         const SeqCaches& kv = k ? b.own : b.pre;
         const Part pt = open(k);
@@ -750,19 +704,19 @@ __global__ __launch_bounds__(kNT, 2 / kRW) void attend_wide_kernel(AttendArgs ar
           for (int ks = 0; ks < KS; ++ks) {
             const u32x4 kk = ldg_u4(kv.k + at + 16 * ks + 8 * hf2);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x = fmaf(elem<F16>(chunk_elem(kk, j)), elem<F16>(chunk_elem(qf[w][ks], j)), x);
+            for (int j = 0; j < 8; ++j) x = fmaf(elem<F16>(chunk_elem(kk, j)), elem<F16>(chunk_elem(qf[ks], j)), x);
           }
           x = sum32(x) * b.sl2;
-          if (!(t < pt.row_hi[w] && (t >= pt.row_lo[w] || t < pt.rg.n_first))) continue;
-          const float nm = fmaxf(m[w], x), ref = nm == -INFINITY ? 0.f : nm;
-          const float al = __builtin_amdgcn_exp2f(m[w] - ref), p = __builtin_amdgcn_exp2f(x - ref);
-          m[w] = nm;
-          l[w] = l[w] * al + p;
+          if (!(t < pt.row_hi && (t >= pt.row_lo || t < pt.rg.n_first))) continue;
+          const float nm = fmaxf(m, x), ref = nm == -INFINITY ? 0.f : nm;
+          const float al = __builtin_amdgcn_exp2f(m - ref), p = __builtin_amdgcn_exp2f(x - ref);
+          m = nm;
+          l = l * al + p;
 #pragma unroll
           for (int db = 0; db < DB; ++db)
 #pragma unroll
             for (int r = 0; r < 16; ++r)
-              o[w][db][r] = fmaf(p, elem<F16>(kv.v[at + 32 * db + 8 * (r / 4) + 4 * hf2 + r % 4]), o[w][db][r] * al);
+              o[db][r] = fmaf(p, elem<F16>(kv.v[at + 32 * db + 8 * (r / 4) + 4 * hf2 + r % 4]), o[db][r] * al);
         }
       }
     }
@@ -773,18 +727,16 @@ __global__ __launch_bounds__(kNT, 2 / kRW) void attend_wide_kernel(AttendArgs ar
       const int64_t item = PRE ? (int64_t)blockIdx.x : 2 * (int64_t)blockIdx.x + (goes_on ? 0 : 1);
       if (goes_on) record.w = ends ? 2 : 1;
       else record = make_int4(s2, rb2, 1, record.w);
-#pragma unroll
-      for (int w = 0; w < kRW; ++w) {
-        const int row = (wave * kRW + w) * 32 + c2;
-        if (row >= rows2) continue;
+      const int row = wave * 32 + c2;
+      if (row < rows2) {
         const int64_t at = item * kRB + row;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
           for (int r = 0; r < 16; r += 4)
             *reinterpret_cast<f32x4*>(sp.o + at * D + 32 * db + 2 * r + 4 * hf2) =
-                f32x4{o[w][db][r], o[w][db][r + 1], o[w][db][r + 2], o[w][db][r + 3]};
-        if (hf2 == 0) *reinterpret_cast<float2*>(sp.ml + at * 2) = make_float2(m[w], l[w]);
+                f32x4{o[db][r], o[db][r + 1], o[db][r + 2], o[db][r + 3]};
+        if (hf2 == 0) *reinterpret_cast<float2*>(sp.ml + at * 2) = make_float2(m, l);
       }
       continue;
     }
@@ -793,41 +745,38 @@ __global__ __launch_bounds__(kNT, 2 / kRW) void attend_wide_kernel(AttendArgs ar
     constexpr int kPitch = 2 * D + 16;
     static_assert(kRB * kPitch <= 6 * L::kTileB);
     tile_barrier();                                  // no wave reads tiles any more
+    const int row0 = wave * 32, row = row0 + c2;
+    if (row0 >= rows2) continue;
+    char* mine = tiles + row0 * kPitch;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const float lse = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+    bool bad = l != 0.f && !__builtin_isfinite(lse);
 #pragma unroll
-    for (int w = 0; w < kRW; ++w) {
-      const int row0 = (wave * kRW + w) * 32, row = row0 + c2;
-      if (row0 >= rows2) continue;
-      char* mine = tiles + row0 * kPitch;
-      const float inv = l[w] == 0.f ? 0.f : 1.f / l[w];
-      const float lse = l[w] == 0.f ? -INFINITY : (m[w] + __builtin_amdgcn_logf(l[w])) * kLn2;
-      bool bad = l[w] != 0.f && !__builtin_isfinite(lse);
+    for (int db = 0; db < DB; ++db)
 #pragma unroll
-      for (int db = 0; db < DB; ++db)
+      for (int r = 0; r < 16; r += 4) {
+        float y[4];
 #pragma unroll
-        for (int r = 0; r < 16; r += 4) {
-          float y[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            y[j] = l[w] == 0.f ? 0.f : o[w][db][r + j] * inv;
-            bad |= !__builtin_isfinite(y[j]);
-          }
-          *reinterpret_cast<uint2*>(mine + c2 * kPitch + (32 * db + 2 * r + 4 * hf2) * 2) =
-              make_uint2(pack2<F16>(y[0], y[1]), pack2<F16>(y[2], y[3]));
+        for (int j = 0; j < 4; ++j) {
+          y[j] = l == 0.f ? 0.f : o[db][r + j] * inv;
+          bad |= !__builtin_isfinite(y[j]);
         }
-      if (bad && row < rows2) latch_nonfinite(b.nonfinite);
-      if (b.lse && hf2 == 0 && row < rows2) {
-        const int q = rb2 * kRB + row;
-        b.lse[(int64_t)(r2 + q / b.group) * b.Hq + g * b.group + q % b.group] = lse;
+        *reinterpret_cast<uint2*>(mine + c2 * kPitch + (32 * db + 2 * r + 4 * hf2) * 2) =
+            make_uint2(pack2<F16>(y[0], y[1]), pack2<F16>(y[2], y[3]));
       }
-      wait_lds_reads();                              // the wave's own writes, too
+    if (bad && row < rows2) latch_nonfinite(b.nonfinite);
+    if (b.lse && hf2 == 0 && row < rows2) {
+      const int q = rb2 * kRB + row;
+      b.lse[(int64_t)(r2 + q / b.group) * b.Hq + g * b.group + q % b.group] = lse;
+    }
+    wait_lds_reads();                              // the wave's own writes, too
 #pragma unroll
-      for (int j = 0; j < 32 / L::LANES; ++j) {
-        const int r = j * L::LANES + ln / L::CH, ch2 = ln % L::CH, gr = row0 + r;
-        if (gr < rows2) {
-          const int q = rb2 * kRB + gr;
-          const int64_t out = (int64_t)(r2 + q / b.group) * b.Hq + g * b.group + q % b.group;
-          *reinterpret_cast<u32x4*>(b.o + out * D + ch2 * 8) = *reinterpret_cast<const u32x4*>(mine + r * kPitch + ch2 * 16);
-        }
+    for (int j = 0; j < 32 / L::LANES; ++j) {
+      const int r = j * L::LANES + ln / L::CH, ch2 = ln % L::CH, gr = row0 + r;
+      if (gr < rows2) {
+        const int q = rb2 * kRB + gr;
+        const int64_t out = (int64_t)(r2 + q / b.group) * b.Hq + g * b.group + q % b.group;
+        *reinterpret_cast<u32x4*>(b.o + out * D + ch2 * 8) = *reinterpret_cast<const u32x4*>(mine + r * kPitch + ch2 * 16);
       }
     }
   }
