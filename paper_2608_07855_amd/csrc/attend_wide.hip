@@ -252,7 +252,12 @@ __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, Sp
   // the arguments are read anew: kept in scalar registers through the tiles they
   // spill, and a spilled register's reload inside the loop drains the loads.
   __shared__ volatile int kept[kNW][32];
-  const AttendArgs& a = fresh_args(args);
+  // (One block, and no second part, leave registers enough: PRE keeps both.)
+  auto fresh = [&]() -> const AttendArgs& {
+    if constexpr (PRE) return args;
+    else return fresh_args(args);
+  };
+  const AttendArgs& a = fresh();
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), c = lane & 31, hf = lane >> 5;
   const int g = blockIdx.x % a.Hkv, e = blockIdx.x / a.Hkv;
   const int pre_n = a.has_pre ? uniform(seq_tokens(a.pre, 0)) : 0;
@@ -301,7 +306,7 @@ __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, Sp
   int4 record = make_int4(0, 0, 0, 0);
   for (bool opening = true; me.left > 0; opening = false) {
     if (!opening) tile_barrier();          // the block before is done with LDS
-    const AttendArgs& a = fresh_args(args);
+    const AttendArgs& a = fresh();
     // the share's part of this block
     const int s = me.s, rb = me.rb;
     const int r0 = uniform(row_start(a, PRE ? 0 : s)), R = uniform(row_start(a, PRE ? a.own.n_seq : s + 1)) - r0;
@@ -357,26 +362,28 @@ __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, Sp
       bmin = min(bmin, qlim[0][w]);
       bmax = max(bmax, qlim[1][w]);
     }
-    keep(kS, s);
-    keep(kRb, rb);
-    keep(kR0, r0);
-    keep(kRows, n_rows);
-    keep64(kX0, x0);
-    keep64(kX1, x1);
-    keep64(kWork, work);
-    keep(kQmin, qmin);
-    keep(kQmax, qmax);
-    keep(kBmin, bmin);
-    keep(kBmax, bmax);
-    keep(kNextS, me.s);
-    keep(kNextRb, me.rb);
-    keep64(kNextX, me.x);
-    keep64(kLeft, me.left);
-    keep(kOpening, opening);
-    keep(kRecord, record.x);
-    keep(kRecord + 1, record.y);
-    keep(kRecord + 2, record.z);
-    keep(kRecord + 3, record.w);
+    if constexpr (!PRE) {
+      keep(kS, s);
+      keep(kRb, rb);
+      keep(kR0, r0);
+      keep(kRows, n_rows);
+      keep64(kX0, x0);
+      keep64(kX1, x1);
+      keep64(kWork, work);
+      keep(kQmin, qmin);
+      keep(kQmax, qmax);
+      keep(kBmin, bmin);
+      keep(kBmax, bmax);
+      keep(kNextS, me.s);
+      keep(kNextRb, me.rb);
+      keep64(kNextX, me.x);
+      keep64(kLeft, me.left);
+      keep(kOpening, opening);
+      keep(kRecord, record.x);
+      keep(kRecord + 1, record.y);
+      keep(kRecord + 2, record.z);
+      keep(kRecord + 3, record.w);
+    }
 
     f32x16 o[DB];
     float m = -INFINITY, l = 0.f;
@@ -385,21 +392,28 @@ __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, Sp
     bool hidden = false;          // some tile held tokens that not all rows see
 
     auto open = [&](int k) {
-      const AttendArgs& a = fresh_args(args);
+      const AttendArgs& a = fresh();
       const SeqCaches& kv = k ? a.own : a.pre;
-      const int s = get(kS), qmin = get(kQmin), qmax = get(kQmax), bmin = get(kBmin), bmax = get(kBmax);
+      int w0 = qmin, w1 = qmax, b0 = bmin, b1 = bmax, sq = 0;
+      if constexpr (!PRE) {
+        sq = get(kS);
+        w0 = get(kQmin);
+        w1 = get(kQmax);
+        b0 = get(kBmin);
+        b1 = get(kBmax);
+      }
       Part t;
-      t.sq = k ? s : 0;
+      t.sq = k ? sq : 0;
       t.n = uniform(seq_tokens(kv, t.sq));
       t.base = k ? pre_n : 0;
-      t.rg = seen_range(kv, t.sq, t.n, t.base, bmin, bmax, a.window, a.n_sink);
+      t.rg = seen_range(kv, t.sq, t.n, t.base, b0, b1, a.window, a.n_sink);
       t.rg.ns = uniform(t.rg.ns);
       t.rg.shift = uniform(t.rg.shift);
       t.rg.cnt = uniform(t.rg.cnt);
       t.rg.lo = uniform(t.rg.lo);
       t.rg.hi = uniform(t.rg.hi);
       t.rg.n_first = uniform(t.rg.n_first);
-      const Range all = seen_range(kv, t.sq, t.n, t.base, qmax, qmin, a.window, a.n_sink);   // window of the last, end of the first
+      const Range all = seen_range(kv, t.sq, t.n, t.base, w1, w0, a.window, a.n_sink);   // window of the last, end of the first
       t.full_hi = uniform(all.hi);
       t.full_lo = uniform(all.lo);
       if (kv.pos) {
@@ -435,7 +449,7 @@ __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, Sp
 
     const bool has_pre = a.has_pre;
     for (int k = has_pre ? 0 : 1; k < (PRE ? 1 : 2); ++k) {
-      const AttendArgs& a = fresh_args(args);
+      const AttendArgs& a = fresh();
       const SeqCaches& kv = k ? a.own : a.pre;
       const Part pt = open(k);
       const float sl2 = a.sl2;
@@ -672,11 +686,20 @@ __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, Sp
     int ln = lane;
     asm volatile("" : "+v"(ln));
     const int c2 = ln & 31, hf2 = ln >> 5;
-    const AttendArgs& b = fresh_args(args);
-    const int s2 = get(kS), rb2 = get(kRb), r2 = get(kR0), rows2 = get(kRows);
-    const bool begun = get64(kX0) > 0, ends = get64(kX1) >= get64(kWork), first = get(kOpening);
-    me = {get(kNextS), get(kNextRb), get64(kNextX), get64(kLeft), false};
-    record = make_int4(get(kRecord), get(kRecord + 1), get(kRecord + 2), get(kRecord + 3));
+    const AttendArgs& b = fresh();
+    int s2 = s, rb2 = rb, r2 = r0, rows2 = n_rows;
+    bool begun = true, ends = true, first = true;
+    if constexpr (!PRE) {
+      s2 = get(kS);
+      rb2 = get(kRb);
+      r2 = get(kR0);
+      rows2 = get(kRows);
+      begun = get64(kX0) > 0;
+      ends = get64(kX1) >= get64(kWork);
+      first = get(kOpening);
+      me = {get(kNextS), get(kNextRb), get64(kNextX), get64(kLeft), false};
+      record = make_int4(get(kRecord), get(kRecord + 1), get(kRecord + 2), get(kRecord + 3));
+    }
     l = sum32(l);
     // A token that only some rows of the block see has weight 0 in the others,
     // and 0 times a value that is not finite is NaN: then the share's tokens
