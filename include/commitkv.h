@@ -600,8 +600,8 @@ typedef struct ckv_query_view {
  * Values, keys and slots of tokens that no row of a sequence sees do not
  * reach its outputs, whatever they hold.
  * Precision: float32 logits, maxima, sums and accumulation; softmax weights
- * rounded to the batch's type before they multiply the values (up to 32 rows a
- * sequence and KV head: to two values of the type, weight and rest).
+ * rounded to the batch's type before they multiply the values (where few rows
+ * read a cache: to two values of the type, weight and rest).
  *
  * The call reads counts and lengths on the device only, so a captured step
  * replays with grown caches.  Partial sums live in a workspace of the context
@@ -609,7 +609,8 @@ typedef struct ckv_query_view {
  * time need contexts of their own.  Memory a captured graph refers to is kept
  * until ckv_destroy (it counts toward ckv_workspace_bytes and the limit of
  * ckv_set_workspace_limit), and an equal call made before the capture (the same
- * n_seq, n_rows, max_rows, max_tokens, heads) leaves the workspace it needs.
+ * n_seq, n_rows, max_rows, max_tokens, heads, window and n_sink) leaves the
+ * workspace it needs.
  * Under a workspace limit that leaves no room for partial sums the call runs
  * without splitting sequences (more slowly, the same results up to rounding).
  *

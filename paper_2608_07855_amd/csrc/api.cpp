@@ -1803,6 +1803,27 @@ SeqCaches make_caches(const ckv_batch_view* v) {
   return c;
 }
 
+// Whether a call takes the few-rows kernel, with the rows of all sequences
+// together over the shared tokens before it, or the many-rows kernel over both
+// parts.  The former reads a sequence's tokens once for every 16 of its rows,
+// the latter once for 256, at about the same time a token where 16 rows wait for
+// HBM and 0.7 of it where more find the tokens in L2 (16 sequences of 8192
+// tokens, 8 KV heads: 16 rows 111 and 110 us, 32 rows 187 and 111, 96 rows 483
+// and 126).  So without shared tokens the few-rows kernel has up to 16 rows,
+// and calls so small that its shorter chain of loads decides (64 rows of 4
+// sequences of 512 tokens 15 and 24 us; of 2048 tokens 42 and 30).  With shared
+// tokens the reads of both forms are compared (16 sequences on 16384 shared
+// tokens and 1024 own ones: 96 rows 135 and 215 us; 128 rows on 2048 and 512: 82
+// and 63).
+bool take_few(const AttendArgs& a, int64_t n_pre, int64_t n_own) {
+  const int64_t n = std::min(a.own.n_seq, a.n_rows), rows = (int64_t)a.max_rows * a.group;
+  const double blocks = (double)((rows + 15) / 16), wide = (double)((rows + 255) / 256);
+  if (a.window) n_own = std::min(n_own, (int64_t)a.window + a.n_sink + a.max_rows);
+  if (!a.has_pre) return blocks <= 1 || n * blocks * a.Hkv * n_own <= 512 * 256;
+  const double packed = (double)(((int64_t)a.n_rows * a.group + 255) / 256);
+  return packed * n_pre + n * std::max(1.0, 0.7 * blocks) * n_own <= n * wide * (double)(n_pre + n_own);
+}
+
 int attend(ckv_ctx* c, const ckv_batch_view* pre, const ckv_batch_view* kv, const ckv_query_view* q, int32_t window,
            int32_t n_sink, void* o, float* lse) {
   if (q->n_rows == 0 || kv->n_seq == 0) return CKV_OK;
@@ -1831,11 +1852,7 @@ int attend(ckv_ctx* c, const ckv_batch_view* pre, const ckv_batch_view* kv, cons
   a.o = static_cast<uint16_t*>(o);
   a.lse = lse;
   a.nonfinite = c->nf_dev;
-  // Up to 32 rows a sequence and KV head take the few-rows kernel (blocks of
-  // 16, so K and V are read twice at most, the second time from L2), the rows of
-  // all sequences together over the shared tokens before it.  More rows fill
-  // the matrix units by themselves: they read both parts in one pass.
-  bool few = (int64_t)q->max_rows * a.group <= 32;
+  bool few = take_few(a, pre ? pre->max_tokens : 0, kv->max_tokens);
   AttendPlan p = few ? plan_narrow(a, kv->max_tokens, true) : plan_wide(a, true);
   PrefixPlan pf = {0, 0, 0};
   if (pre && few) pf = plan_prefix(a);

@@ -80,7 +80,7 @@ __global__ __launch_bounds__(64 * NW) void attend_narrow_kernel(AttendArgs a, Sp
   __shared__ int last;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, q = lane >> 4;
   const int g = blockIdx.x % a.Hkv;
-  const Item it = find_item<NT, L::kRows>(a, blockIdx.x / a.Hkv, target, min_chunk, ish);
+  const Item it = find_item<NT, L::kRows>(a, blockIdx.x / a.Hkv, target, min_chunk, NW == 512 / D, ish);
   // (a block whose splits pass the grid, which rows out of order can make, is left
   // by all of them: none counts an arrival that the others do not)
   if (it.s < 0 || (it.e - it.split + it.n_split) * a.Hkv > gridDim.x) return;
@@ -395,10 +395,17 @@ AttendPlan plan_narrow(const AttendArgs& a, int64_t max_tokens, bool room) {
   // lengths differ from block to block, and two rounds even them out.
   p.alone = blocks * a.Hkv <= 256;
   p.target = p.alone ? 256 : 1024;
-  // Joining splits costs about 7 us; a split saves less below this length.
-  p.min_chunk = 2048;
+  // A workgroup takes 17 us for 1000 tokens, and joining splits costs 5-7 us.
+  // Four workgroups a block or more: short splits (one token of a 2048-token
+  // cache 12 us, whole 27; of 4 caches of 4096 tokens 19, with splits of 2048
+  // 31).  Fewer: what halves save the join takes (16 caches, a window of 1024
+  // tokens: whole 14.7, in halves 16.2 us).
+  // (Of `blocks` about two thirds are there.)
+  const bool small = blocks * a.Hkv <= 96;
+  const int64_t seen = a.window ? std::min(max_tokens, (int64_t)a.window + a.n_sink + a.max_rows) : max_tokens;
+  p.min_chunk = small ? 256 : 2048;
   int64_t e = p.target / a.Hkv + blocks + 1;
-  if (!room || max_tokens <= p.min_chunk || blocks * a.Hkv >= 4 * p.target) {
+  if (!room || seen <= (small ? 512 : 2048) || blocks * a.Hkv >= 4 * p.target) {
     p.min_chunk = INT_MAX;                                              // no splits
     e = blocks;
   }

@@ -107,9 +107,10 @@ __device__ __forceinline__ long long wave_scan(long long v) {
 }
 
 // Item e of a KV head: blocks of RB rows, about `target` items over all heads,
-// at least min_chunk tokens each.
+// at least min_chunk tokens each.  one_round: `target` at most (up to 64
+// sequences), as many as run at the same time.
 template <int NT, int RB>
-__device__ __forceinline__ Item find_item(const AttendArgs& a, int64_t e, int target, int min_chunk, ItemShared& sh) {
+__device__ __forceinline__ Item find_item(const AttendArgs& a, int64_t e, int target, int min_chunk, bool one_round, ItemShared& sh) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n_seq = a.own.n_seq;
   auto load = [&](int s, int& nrb, int& est) {
     nrb = est = 0;
@@ -133,8 +134,19 @@ __device__ __forceinline__ Item find_item(const AttendArgs& a, int64_t e, int ta
     if (min_chunk != INT_MAX)
 #pragma unroll
       for (int off = 32; off; off >>= 1) work += __shfl_xor(work, off, 64);
-    const int n_split = splits(est, chunk_of(work));
-    const long long mine = (long long)nrb * n_split, at = e - (wave_scan(mine) - mine);
+    int n_split = splits(est, chunk_of(work));
+    long long mine = (long long)nrb * n_split, upto = wave_scan(mine);
+    if (one_round && min_chunk != INT_MAX && __shfl(upto, 63, 64) * a.Hkv > target) {
+      // rounded up, the splits are too many: at most one a block more than this chunk gives
+      int blocks = nrb;
+#pragma unroll
+      for (int off = 32; off; off >>= 1) blocks += __shfl_xor(blocks, off, 64);
+      const int left = max(target / a.Hkv - blocks, 1);
+      n_split = splits(est, max((int64_t)min_chunk, (int64_t)((work + left - 1) / left)));
+      mine = (long long)nrb * n_split;
+      upto = wave_scan(mine);
+    }
+    const long long at = e - (upto - mine);
     const unsigned long long who = __ballot(at >= 0 && at < mine);
     const int s = who ? __ffsll(who) - 1 : 0;
     it.s = who ? s : -1;

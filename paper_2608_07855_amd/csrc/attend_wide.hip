@@ -289,7 +289,7 @@ __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, Sp
     whole = me.whole;
     if (sp.share && e < W && tid == 0 && (whole || me.s < 0)) sp.share[blockIdx.x] = make_int4(0, 0, 0, 0);
     if (whole) {
-      const Item it = find_item<kNT, kRB>(a, e, 1, INT_MAX, ssh.item);
+      const Item it = find_item<kNT, kRB>(a, e, 1, INT_MAX, false, ssh.item);
       me = {it.s, it.rb, 0, 1, true};
     }
     if (me.s < 0) return;
