@@ -14,8 +14,8 @@
 // any order between its workgroups: each forms the prefix sums for itself (a
 // few thousand lengths, from L2) and takes a share of the pieces, returned
 // blocks and sequences.  A thread writes a piece's tokens, up to four words a
-// store (a thread per token spent its time finding each token's sequence:
-// 1024 prompts 16.6 us).
+// store (1024 prompts, 920K tokens, 13.5 us; a thread per token spent its time
+// finding each token's sequence: 16.6).
 //
 // Bound: latency.  A step reads two counts a sequence, moves two words a
 // block and writes four words a token.
