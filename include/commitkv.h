@@ -657,11 +657,13 @@ typedef struct ckv_slot_step {
   const int32_t* n_free;       /* int32[1]: free blocks */
   /* updated in place */
   int32_t* free_blocks;        /* int32[n_blocks]: stack of free blocks, top last */
-  int32_t* block_table;        /* int32 [n_seq][block_stride], or NULL with block_size 1 */
-  int64_t block_stride;
-  int32_t* slot;               /* int32 [n_seq][slot_stride]: pool row of each token */
-  int32_t* pos;                /* int32 [n_seq][slot_stride], or NULL */
-  int64_t slot_stride;
+  int32_t* block_table;        /* int32 [n_seq][block_cols], or NULL with block_size 1 */
+  int64_t block_stride;        /* entries between two rows, block_cols or more */
+  int64_t block_cols;
+  int32_t* slot;               /* int32 [n_seq][slot_cols]: pool row of each token */
+  int32_t* pos;                /* int32 [n_seq][slot_cols], or NULL */
+  int64_t slot_stride;         /* of slot and pos, slot_cols or more */
+  int64_t slot_cols;
   /* outputs; none may overlap an input */
   int32_t* n_tokens_out;       /* int32[n_seq] */
   int32_t* n_free_out;         /* int32[1] */
@@ -674,7 +676,7 @@ typedef struct ckv_slot_step {
 /* ckv_slot_step.status */
 #define CKV_SLOTS_OK 0
 #define CKV_SLOTS_NO_BLOCKS 1  /* the step needs more blocks than are free */
-#define CKV_SLOTS_TABLE 2      /* a sequence would pass slot_stride or block_stride * block_size */
+#define CKV_SLOTS_TABLE 2      /* a sequence would pass slot_cols or block_cols * block_size */
 #define CKV_SLOTS_MAX_NEW 3    /* more than max_new new tokens */
 #define CKV_SLOTS_BAD_COUNT 4  /* a negative n_tokens, an n_new below -1, n_free outside [0, n_blocks] */
 
@@ -701,7 +703,7 @@ typedef struct ckv_slot_step {
  * several reasons hold, status names the one of highest number.  The result
  * does not depend on scheduling.  Block numbers outside the pool are clamped
  * into it wherever a row is formed.
- * Errors: CKV_ERR_ARG (NULL pointers, block_size or sizes out of range,
+ * Errors: CKV_ERR_ARG (NULL pointers, block_size, strides or sizes out of range,
  * block_table missing where block_size > 1, outputs that overlap inputs or
  * each other: a table counts from its first to its last row, so tables whose
  * rows alternate in one buffer overlap).

@@ -109,9 +109,9 @@ class SlotStep(ctypes.Structure):
     _fields_ = [("n_seq", ctypes.c_int32), ("block_size", ctypes.c_int32), ("n_blocks", ctypes.c_int32),
                 ("max_new", ctypes.c_int32), ("n_tokens", ctypes.c_void_p), ("n_new", ctypes.c_void_p),
                 ("next_pos", ctypes.c_void_p), ("n_free", ctypes.c_void_p), ("free_blocks", ctypes.c_void_p),
-                ("block_table", ctypes.c_void_p), ("block_stride", ctypes.c_int64), ("slot", ctypes.c_void_p),
-                ("pos", ctypes.c_void_p), ("slot_stride", ctypes.c_int64), ("n_tokens_out", ctypes.c_void_p),
-                ("n_free_out", ctypes.c_void_p), ("cu_new", ctypes.c_void_p), ("new_row", ctypes.c_void_p),
+                ("block_table", ctypes.c_void_p), ("block_stride", ctypes.c_int64), ("block_cols", ctypes.c_int64),
+                ("slot", ctypes.c_void_p), ("pos", ctypes.c_void_p), ("slot_stride", ctypes.c_int64),
+                ("slot_cols", ctypes.c_int64), ("n_tokens_out", ctypes.c_void_p), ("n_free_out", ctypes.c_void_p), ("cu_new", ctypes.c_void_p), ("new_row", ctypes.c_void_p),
                 ("new_pos", ctypes.c_void_p), ("status", ctypes.c_void_p)]
 
 

@@ -334,11 +334,11 @@ def slot_step(n_tokens, n_new, free, n_free, slot, *, block_size: int, block_tab
 
     def p(t):
         return None if t is None else t.data_ptr()
-    # a table of one sequence may have any row stride: its width is what counts
-    def stride(t):
-        return 0 if t is None else (t.stride(0) if t.shape[0] > 1 else t.shape[1])
+
+    def rows(t):
+        return (0, 0) if t is None else (t.stride(0), t.shape[1])
     step = SlotStep(n, int(block_size), free.numel(), int(max_new), p(n_tokens), p(n_new), p(next_pos), p(n_free),
-                    p(free), p(block_table), stride(block_table), p(slot), p(pos), stride(slot), p(n_tokens_out),
+                    p(free), p(block_table), *rows(block_table), p(slot), p(pos), *rows(slot), p(n_tokens_out),
                     p(n_free_out), p(cu_new), p(new_row), p(new_pos), p(status))
     step._keep = (n_tokens, n_new, next_pos, n_free, free, block_table, slot, pos)
     step._device = dev

@@ -1944,10 +1944,18 @@ extern "C" int ckv_build_slots(ckv_ctx* c, const ckv_slot_step* st) {
     return fail(c, CKV_ERR_ARG, "slots: NULL pointer");
   if (n > 0 && !st->block_table && st->block_size != 1)
     return fail(c, CKV_ERR_ARG, "slots: block_table may be NULL with block_size 1 only");
-  if (st->slot_stride < 0 || st->block_stride < 0 || st->slot_stride > INT_MAX || st->block_stride > INT_MAX)
-    return fail(c, CKV_ERR_ARG, "slots: table strides out of range");
+  if (n > 0) {
+    const bool tab = st->block_table != nullptr;
+    if (st->slot_cols < 0 || st->slot_cols > INT_MAX || (tab && (st->block_cols < 0 || st->block_cols > INT_MAX)))
+      return fail(c, CKV_ERR_ARG, "slots: table widths out of range");
+    if (n > 1 && (st->slot_stride < st->slot_cols || st->slot_stride > INT_MAX ||
+                  (tab && (st->block_stride < st->block_cols || st->block_stride > INT_MAX))))
+      return fail(c, CKV_ERR_ARG, "slots: table strides out of range");
+  }
   struct Range { const void* p; size_t n; };
-  const size_t word = 4, tab = (size_t)n * st->slot_stride * word, btab = (size_t)n * st->block_stride * word;
+  const size_t word = 4;
+  auto table_bytes = [&](int64_t stride, int64_t cols) { return n > 0 ? ((size_t)(n > 1 ? (n - 1) * stride : 0) + cols) * word : 0; };
+  const size_t tab = table_bytes(st->slot_stride, st->slot_cols), btab = table_bytes(st->block_stride, st->block_cols);
   const Range in[] = {{st->n_tokens, n * word}, {st->n_new, n * word}, {st->next_pos, n * word}, {st->n_free, word}};
   const Range out[] = {{st->free_blocks, st->n_blocks * word}, {st->block_table, btab}, {st->slot, tab}, {st->pos, tab},
                        {st->n_tokens_out, n * word}, {st->n_free_out, word}, {st->cu_new, (n + 1) * word},
@@ -1972,9 +1980,11 @@ extern "C" int ckv_build_slots(ckv_ctx* c, const ckv_slot_step* st) {
   a.free_blocks = st->free_blocks;
   a.block_table = st->block_table;
   a.block_stride = st->block_stride;
+  a.block_cols = st->block_cols;
   a.slot = st->slot;
   a.pos = st->pos;
   a.slot_stride = st->slot_stride;
+  a.slot_cols = st->slot_cols;
   a.n_tokens_out = st->n_tokens_out;
   a.n_free_out = st->n_free_out;
   a.cu_new = st->cu_new;

@@ -452,7 +452,7 @@ struct SlotArgs {
   int n_seq, block_size, n_blocks, max_new;
   const int32_t *n_tokens, *n_new, *next_pos, *n_free;
   int32_t *free_blocks, *block_table, *slot, *pos;
-  int64_t block_stride, slot_stride;
+  int64_t block_stride, block_cols, slot_stride, slot_cols;
   int32_t *n_tokens_out, *n_free_out, *cu_new, *new_row, *new_pos, *status;
 };
 hipError_t launch_slots(const SlotArgs& a, hipStream_t s);

@@ -141,7 +141,7 @@ __global__ __launch_bounds__(kNT) void slots_kernel(SlotArgs a) {
   const int n_units = (a.n_seq + unit - 1) / unit;
   const int per = (n_units + kNT - 1) / kNT;           // units of a thread
   const int u0 = min(tid * per, n_units), u1 = min(u0 + per, n_units);
-  const int64_t cols = a.block_table ? a.block_stride : a.slot_stride;
+  const int64_t cols = a.block_table ? a.block_cols : a.slot_cols;
   const int shift = (B & (B - 1)) == 0 ? __ffs(B) - 1 : -1;
   if (tid == 0) sh.status = CKV_SLOTS_OK;
   const int nf = *a.n_free;
@@ -154,7 +154,7 @@ __global__ __launch_bounds__(kNT) void slots_kernel(SlotArgs a) {
       return;
     }
     const unsigned now = (unsigned)old + (unsigned)max(nn, 0);
-    if (now > a.slot_stride || blocks_of(now, B, shift) > cols) bad = max(bad, CKV_SLOTS_TABLE);
+    if (now > a.slot_cols || blocks_of(now, B, shift) > cols) bad = max(bad, CKV_SLOTS_TABLE);
   };
   if (unit == 1) {
     // lengths to LDS, eight loads of a thread under way; then each thread sums

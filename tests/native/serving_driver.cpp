@@ -86,9 +86,9 @@ int main() {
   st.n_new = n_new;
   st.n_free = n_free;
   st.free_blocks = dev(stack);
-  st.block_stride = most / B;
+  st.block_stride = st.block_cols = most / B;
   st.block_table = dev(std::vector<int32_t>(N * most / B));
-  st.slot_stride = most;
+  st.slot_stride = st.slot_cols = most;
   st.slot = dev(std::vector<int32_t>(N * most));
   st.pos = dev(std::vector<int32_t>(N * most));
   st.n_tokens_out = dev(std::vector<int32_t>(N));

@@ -190,6 +190,25 @@ def test_captured_steps(ckv):
         ctx.close()
 
 
+def test_columns_of_wider_tables(ckv):
+    """Tables that are columns of wider ones: a step past their width changes nothing beside them."""
+    P, ctx = ckv
+    B, nb = 4, 40
+    wide_slot, wide_tab = _dev(np.full((2, 20), -1)), _dev(np.full((2, 9), -1))
+    slot, tab = wide_slot[:, 12:], wide_tab[:, 6:]
+    for new, want in (((8, 8), 0), ((1, 0), 2), ((0, 9), 2)):
+        st = P.slot_step(_dev([0, 0]) if want == 0 else _dev([8, 8] if new[0] else [8, 0]), _dev(new),
+                         _dev(np.arange(nb)), _dev([nb]), slot, block_size=B, block_table=tab, max_new=32)
+        assert int(P.ckv_build_slots(ctx, st)["status"]) == want
+    st = P.slot_step(_dev([0, 0]), _dev([0, 0]), _dev(np.arange(nb)), _dev([nb]), slot, block_size=B, block_table=tab, max_new=32)
+    st.slot_stride = 7
+    with pytest.raises(P.CKVError) as e:
+        P.ckv_build_slots(ctx, st)
+    assert e.value.code == -1
+    assert wide_slot[:, 12:].min() >= 0 and torch.all(wide_slot[:, :12] == -1) and torch.all(wide_tab[:, :6] == -1)
+    assert wide_tab[:, 6:8].min() >= 0 and torch.all(wide_tab[:, 8] == -1)
+
+
 def test_refusals(ckv):
     P, ctx = ckv
     n, B, nb = 3, 4, 20
