@@ -210,17 +210,19 @@ __global__ __launch_bounds__(64 * NW) void attend_narrow_kernel(AttendArgs a, Sp
     }
     const float ref = m == -INFINITY ? 0.f : m;
     u32x4 ph, pl;
+    float lt = 0.f;               // the tile's sum: small weights add up before they meet a large l
 #pragma unroll
     for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
       for (int r = 0; r < 4; r += 2) {
         const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[tb][r], a.sl2, -ref));
         const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[tb][r + 1], a.sl2, -ref));
-        l += p0 + p1;
+        lt += p0 + p1;
         const uint16_t h0 = to_elem<F16>(p0), h1 = to_elem<F16>(p1);
         ph[2 * tb + r / 2] = h0 | (uint32_t)h1 << 16;
         pl[2 * tb + r / 2] = to_elem<F16>(p0 - elem<F16>(h0)) | (uint32_t)to_elem<F16>(p1 - elem<F16>(h1)) << 16;
       }
+    l += lt;
 #pragma unroll
     for (int db = 0; db < D / 16; ++db) {
       u32x4 vf;

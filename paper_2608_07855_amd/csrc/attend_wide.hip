@@ -559,6 +559,7 @@ __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, Sp
         }
         const float ref = m == -INFINITY ? 0.f : m;
         u32x4 ph[4];
+        float lt = 0.f;       // the tile's sum: small weights add up before they meet a large l
         {
           // past the last tile: what an older tile left, used by nobody
           const uint32_t off = ((t + 1) % 3) * L::kTileB;
@@ -577,11 +578,12 @@ __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, Sp
               const int tb = q / 8, r = 2 * (q % 8);
               const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[tb][r], sl2, -ref));
               const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[tb][r + 1], sl2, -ref));
-              l += p0 + p1;
+              lt = q ? lt + (p0 + p1) : p0 + p1;
               ph[q / 4][q % 4] = pack2<F16>(p0, p1);
             }
             __builtin_amdgcn_sched_barrier(0);
           }
+          l += lt;
           // keeps the weights here, beside the products
 #pragma unroll
           for (int j = 0; j < 4; ++j) asm volatile("" : "+v"(ph[j]));
