@@ -601,7 +601,8 @@ typedef struct ckv_query_view {
  * reach its outputs, whatever they hold.
  * Precision: float32 logits, maxima, sums and accumulation; softmax weights
  * rounded to the batch's type before they multiply the values (where few rows
- * read a cache: to two values of the type, weight and rest).
+ * read a cache: to two values of the type, weight and rest).  An fp16 weight
+ * below 2^-27 of a row's largest has fewer bits, and is off by 2^-38 of that at most.
  *
  * The call reads counts and lengths on the device only, so a captured step
  * replays with grown caches.  Partial sums live in a workspace of the context

@@ -56,8 +56,14 @@ __device__ __forceinline__ float sum_rows16(float v) {
 //
 // Softmax weights are split into two values of the type (rounded weight and
 // rounded rest), both multiplied: the matrix units have time for it, and the
-// output keeps the precision of its own rounding.
+// output keeps the precision of its own rounding.  fp16 has no values below 2^-25,
+// and behind a dominant token many smaller weights make up the output: there they
+// are formed 2^15 times as large, and those down to 2^-29 of the largest keep their
+// bits (a smaller one is off by 2^-40 of it at most).
 // ---------------------------------------------------------------------------
+template <bool F16>
+constexpr int kNarrowLog = F16 ? 15 : 0;            // weights are formed this many powers of two as large
+
 template <int D, int NW_>
 struct Narrow {
   static constexpr int NW = NW_, NT = 64 * NW;
@@ -208,7 +214,7 @@ __global__ __launch_bounds__(64 * NW) void attend_narrow_kernel(AttendArgs a, Sp
       for (int db = 0; db < D / 16; ++db) o[db] *= al;
       m = nm;
     }
-    const float ref = m == -INFINITY ? 0.f : m;
+    const float ref = (m == -INFINITY ? 0.f : m) - kNarrowLog<F16>;
     u32x4 ph, pl;
     float lt = 0.f;               // the tile's sum: small weights add up before they meet a large l
 #pragma unroll
@@ -273,6 +279,12 @@ __global__ __launch_bounds__(64 * NW) void attend_narrow_kernel(AttendArgs a, Sp
   }
   wait_loads<0>();
   wait_lds_reads();
+  if constexpr (kNarrowLog<F16> > 0) {
+    constexpr float back = 1.f / (1 << kNarrowLog<F16>);
+    l *= back;
+#pragma unroll
+    for (int db = 0; db < D / 16; ++db) o[db] *= back;
+  }
 
   // A token that only some rows of the block see has weight 0 in the others,
   // and 0 times a value that is not finite is NaN: then the wave's tokens are

@@ -21,8 +21,13 @@ namespace {
 // V^T in that order.
 //
 // The reference of the softmax weights follows a row's largest logit only
-// when that passes it by 2^8 (weights up to 256 keep their relative precision
-// in either type, sums are float32), so that the output is rarely rescaled.
+// when that passes it by 2^kLag, so that the output is rarely rescaled (sums are
+// float32).  In bf16 a weight of any size has 8 bits.  fp16 has 11 from 2^-14 to
+// 2^16 and none below 2^-25, and behind a dominant token many smaller weights make
+// up the output: so they are formed 2^kWeightLog times as large, up to 2^15, and
+// those down to 2^-27 of the largest keep their bits (a smaller one is off by
+// 2^-38 of it at most).  A lag of 8 would leave 2^-21 and saves 1% at best (16
+// fp16 chunks behind a 16K prefix 760, with a lag of 4 763, of 2 769 us).
 //
 // Bound: matrix and vector issue.  A step is 32 products (1024 cycles) and about
 // 140 vector instructions a wave; both waves of a SIMD pass the same barrier a
@@ -38,7 +43,10 @@ namespace {
 // adds.  (Blocks as items of their own left the device idle at the end: 8
 // ragged chunks 323 us, in shares 312, and 290 since nothing spills.)
 // ---------------------------------------------------------------------------
-constexpr float kLag = 8.f;   // log2 units
+template <bool F16>
+constexpr int kLag = F16 ? 2 : 8;                      // log2 units
+template <bool F16>
+constexpr int kWeightLog = F16 ? 15 - kLag<F16> : 0;
 constexpr int kAhead = 4;     // operands read from LDS ahead of their products
 constexpr int kNW = 8, kNT = 64 * kNW, kRB = 256, kTok = 64;
 
@@ -549,7 +557,7 @@ __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, Sp
       // early; the fences keep the compiler from gathering either.
       auto step = [&](int t, f32x16 (&x)[2], float& mx, f32x16 (&y)[2], float& my) {
         const float top = max32(mx) * sl2;
-        if (__ballot(top > m + kLag || (m == -INFINITY && top > m)) != 0ull) {
+        if (__ballot(top > m + kLag<F16> || (m == -INFINITY && top > m)) != 0ull) {
           const float nm = top > m ? top : m;
           const float al = nm == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - nm);
           l *= al;
@@ -557,7 +565,7 @@ __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, Sp
           for (int db = 0; db < DB; ++db) o[db] *= al;
           m = nm;
         }
-        const float ref = m == -INFINITY ? 0.f : m;
+        const float ref = (m == -INFINITY ? 0.f : m) - kWeightLog<F16>;
         u32x4 ph[4];
         float lt = 0.f;       // the tile's sum: small weights add up before they meet a large l
         {
@@ -707,6 +715,12 @@ __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, Sp
       record = make_int4(get(kRecord), get(kRecord + 1), get(kRecord + 2), get(kRecord + 3));
     }
     l = sum32(l);
+    if constexpr (kWeightLog<F16> > 0) {
+      constexpr float back = 1.f / (1 << kWeightLog<F16>);
+      l *= back;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) o[db] *= back;
+    }
     // A token that only some rows of the block see has weight 0 in the others,
     // and 0 times a value that is not finite is NaN: then the share's tokens
     // are taken again one by one, each by the rows that see it.

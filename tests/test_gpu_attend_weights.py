@@ -12,6 +12,14 @@ D = 64
 
 
 @pytest.fixture(scope="module")
+def ckv():
+    import paper_2608_07855_amd as P
+    ctx = P.Context(0)
+    yield P, ctx
+    ctx.close()
+
+
+@pytest.fixture(scope="module")
 def limited():
     """A context without room for partial sums: nothing is split."""
     import paper_2608_07855_amd as P
@@ -61,10 +69,11 @@ class Dominated:
 def _check(case, got, want, what):
     """Values are not negative, so that a relative error of every weight is one of the output.  Half a step of the type
     for the output's rounding, as much for the weights', and 2^-13 for the logits, exponentials and sums in float32
-    (an absolute error in lse)."""
+    (an absolute error in lse).  An fp16 weight may be off by 2^-38 of the largest one as well, n of them."""
     (o, lse), (wo, wl) = got, want
     h = HALF[case.type]
-    eo, el = np.abs(o - wo) / ((2 * h + 2.0**-13) * wo), np.abs(lse - wl) / (2.0**-13 + 2.0**-22 * wl)
+    far = case.n * 2.0**-38 * 1.5 if case.type == "fp16" else 0.0
+    eo, el = np.abs(o - wo) / ((2 * h + 2.0**-13) * wo + far), np.abs(lse - wl) / (2.0**-13 + 2.0**-22 * wl)
     print(f"[parity] {what}: o {eo.max():.3g}, lse {el.max():.3g} of the tolerance", flush=True)
     assert eo.max() <= 1 and el.max() <= 1, what
 
@@ -76,3 +85,15 @@ def test_sums_without_splits(limited, n, rows):
     P, ctx = limited
     c = Dominated(n + 1, rows, "bf16", gaps=[12.0, 16.6, 17.0, 17.4, 18.0])
     _check(c, c.run(P, ctx), c.want(), f"{n} tokens, {rows} rows")
+
+
+@pytest.mark.parametrize("type", ["bf16", "fp16"])
+@pytest.mark.parametrize("rows", [1, 64])
+@pytest.mark.parametrize("prefix", [0, 131008])
+@pytest.mark.parametrize("split", [True, False])
+def test_many_small_weights(ckv, limited, split, rows, prefix, type):
+    """131072 tokens behind a dominant one: few and many rows, over one cache and over a shared prefix, in splits (of
+    which one alone holds the dominant token) and whole."""
+    P, ctx = ckv if split else limited
+    c = Dominated(131073, rows, type, prefix, gaps=[12.0, 16.6, 17.0, 18.0])
+    _check(c, c.run(P, ctx), c.want(), f"{rows} rows, prefix {prefix}")
