@@ -96,9 +96,10 @@ struct ckv_ctx {
   // single calls have been recorded with (a captured graph of them).
   struct Arena { char* p = nullptr; size_t cap = 0; };
   Arena ws, batch_ws;
-  // Split partials and arrival counts of the attention calls.  Captured graphs
-  // refer to it, so what it outgrows is kept until the context goes.
+  // Split partials and arrival counts of the attention calls.  What a call was
+  // recorded with (a captured graph refers to it) is kept until the context goes.
   Arena attend_ws;
+  bool attend_captured = false;
   std::vector<Arena> outgrown;
   size_t outgrown_bytes = 0;
   size_t ws_limit = 0;   // of both together
@@ -228,7 +229,7 @@ bool allocate(ckv_ctx::Arena& a, size_t bytes) {
   return true;
 }
 
-// what the attention calls hold: captured graphs may refer to it, so nothing frees it
+// what the attention calls hold: the other calls leave it alone
 size_t attend_held(const ckv_ctx* c) { return c->attend_ws.cap + c->outgrown_bytes; }
 
 int ensure_ws(ckv_ctx* c, size_t need) {
@@ -267,41 +268,53 @@ int ensure_batch_ws(ckv_ctx* c, size_t need) {
   return fail(c, CKV_ERR_NOMEM, "hipMalloc of %zu workspace bytes failed", need);
 }
 
+bool capturing(ckv_ctx* c) {
+  hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(c->stream, &st) == hipSuccess) return st != hipStreamCaptureStatusNone;
+  (void)hipGetLastError();
+  return true;
+}
+
 // Room for the attention calls: arrival counts (zero between calls) in the
 // first kAttendCounts bytes, split partials behind them.  *room is false where
-// the workspace limit leaves none.  No stream is waited for: what is outgrown
-// stays where it is, for work under way and for captured graphs.
+// the workspace limit leaves none.  Under a limit nothing is taken in advance, so
+// that what attention has grown to leaves the other calls the rest.
 int ensure_attend_ws(ckv_ctx* c, size_t part, bool* room) {
   const size_t need = kAttendCounts + part;
+  const bool recorded = capturing(c), grow = need > c->attend_ws.cap;
   *room = true;
-  if (need <= c->attend_ws.cap) return CKV_OK;
-  const size_t held = c->ws.cap + c->batch_ws.cap + attend_held(c);
-  size_t want = std::max(need, 2 * c->attend_ws.cap);
-  if (c->ws_limit) {
-    const size_t left = c->ws_limit - std::min(c->ws_limit, held);
-    *room = need <= left;
-    if (!*room) return CKV_OK;
-    want = std::min(want, left);
+  if (grow) {
+    const size_t kept = c->attend_captured ? c->attend_ws.cap : 0;
+    if (c->ws_limit) {
+      const size_t held = c->ws.cap + c->batch_ws.cap + c->outgrown_bytes + kept;
+      *room = held <= c->ws_limit && need <= c->ws_limit - held;
+      if (!*room) return CKV_OK;
+    }
+    if (recorded)
+      return fail(c, CKV_ERR_NOMEM, "the workspace has to grow to %zu bytes, which a capture cannot record: make an equal call before it", need);
+    if (c->attend_captured) {
+      try {
+        c->outgrown.push_back(c->attend_ws);
+      } catch (const std::bad_alloc&) {
+        return fail(c, CKV_ERR_NOMEM, "out of host memory");
+      }
+      c->outgrown_bytes += kept;
+      c->attend_ws = ckv_ctx::Arena();
+      c->attend_captured = false;
+    }
+    const size_t want = c->ws_limit ? need : std::max(need, 2 * c->attend_ws.cap);
+    CKV_HIP(c, hipStreamSynchronize(c->stream));   // in-flight work may still use the old arena
+    release(c->attend_ws);
+    ckv_ctx::Arena a;
+    if (!allocate(a, want) && !allocate(a, need)) return fail(c, CKV_ERR_NOMEM, "hipMalloc of %zu workspace bytes failed", need);
+    const hipError_t e = hipMemsetAsync(a.p, 0, kAttendCounts, c->stream);
+    if (e != hipSuccess) {
+      release(a);
+      return hip_fail(c, e, "hipMemsetAsync of the arrival counts");
+    }
+    c->attend_ws = a;
   }
-  hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
-  CKV_HIP(c, hipStreamIsCapturing(c->stream, &st));
-  if (st != hipStreamCaptureStatusNone)
-    return fail(c, CKV_ERR_NOMEM, "the workspace has to grow to %zu bytes, which a capture cannot record: make an equal call before it", need);
-  ckv_ctx::Arena a;
-  if (!allocate(a, want) && !allocate(a, need)) return fail(c, CKV_ERR_NOMEM, "hipMalloc of %zu workspace bytes failed", need);
-  const hipError_t e = hipMemsetAsync(a.p, 0, kAttendCounts, c->stream);
-  if (e != hipSuccess) {
-    release(a);
-    return hip_fail(c, e, "hipMemsetAsync of the arrival counts");
-  }
-  try {
-    if (c->attend_ws.p) c->outgrown.push_back(c->attend_ws);
-  } catch (const std::bad_alloc&) {
-    release(a);
-    return fail(c, CKV_ERR_NOMEM, "out of host memory");
-  }
-  c->outgrown_bytes += c->attend_ws.cap;
-  c->attend_ws = a;
+  if (recorded) c->attend_captured = true;
   return CKV_OK;
 }
 
@@ -1036,13 +1049,6 @@ int enqueue_batch(ckv_ctx* c, const BatchItem* it, int n, const BatchTables& tab
   }
   if (it[0].mass) CKV_LAUNCH(c, b.mass_fixup ? "token_mass_fixup" : "token_mass", launch_measure_batch(dev, b, 4, c->stream));
   return CKV_OK;
-}
-
-bool capturing(ckv_ctx* c) {
-  hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
-  if (hipStreamIsCapturing(c->stream, &st) == hipSuccess) return st != hipStreamCaptureStatusNone;
-  (void)hipGetLastError();
-  return true;
 }
 
 // Records problems it[0 .. n) one after another.  The arguments of a run are
