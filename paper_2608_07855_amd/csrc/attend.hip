@@ -168,6 +168,7 @@ __global__ __launch_bounds__(64 * NW) void attend_narrow_kernel(AttendArgs a, Sp
 #pragma unroll
   for (int db = 0; db < D / 16; ++db) o[db] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = 0.f;
+  bool large = false;                        // a row's m is: see kLargeRef
   auto compute = [&](int tile) {
     const uint32_t kb = my + (tile & 1) * 2 * L::kTileB, vb = kb + L::kTileB;
     f32x4 x[2];
@@ -213,16 +214,26 @@ __global__ __launch_bounds__(64 * NW) void attend_narrow_kernel(AttendArgs a, Sp
 #pragma unroll
       for (int db = 0; db < D / 16; ++db) o[db] *= al;
       m = nm;
+      large = any_large(m);
     }
-    const float ref = (m == -INFINITY ? 0.f : m) - kNarrowLog<F16>;
+    float ref = m == -INFINITY ? 0.f : m, sl2 = a.sl2;
+    if (__builtin_expect(large, 0)) {
+#pragma unroll
+      for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[tb][r] = product(x[tb][r], sl2) - ref;
+      ref = 0.f;
+      sl2 = 1.f;
+    }
+    ref -= kNarrowLog<F16>;
     u32x4 ph, pl;
     float lt = 0.f;               // the tile's sum: small weights add up before they meet a large l
 #pragma unroll
     for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
       for (int r = 0; r < 4; r += 2) {
-        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[tb][r], a.sl2, -ref));
-        const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[tb][r + 1], a.sl2, -ref));
+        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[tb][r], sl2, -ref));
+        const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[tb][r + 1], sl2, -ref));
         lt += p0 + p1;
         const uint16_t h0 = to_elem<F16>(p0), h1 = to_elem<F16>(p1);
         ph[2 * tb + r / 2] = h0 | (uint32_t)h1 << 16;
@@ -310,7 +321,7 @@ __global__ __launch_bounds__(64 * NW) void attend_narrow_kernel(AttendArgs a, Sp
 #pragma unroll
           for (int e = 0; e < 8; ++e) x = fmaf(elem<F16>(chunk_elem(kk, e)), elem<F16>(chunk_elem(qf[ks], e)), x);
         }
-        x = sum_rows16(x) * a.sl2;
+        x = product(sum_rows16(x), a.sl2);
         if (!sees(poss ? poss[t] : base + t, qp, a.window, a.n_sink)) continue;
         const float nm = fmaxf(m, x), ref = nm == -INFINITY ? 0.f : nm;
         const float al = __builtin_amdgcn_exp2f(m - ref), w = __builtin_amdgcn_exp2f(x - ref);

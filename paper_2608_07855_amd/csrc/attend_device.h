@@ -40,6 +40,21 @@ __device__ __forceinline__ bool sees(int p, int qp, int window, int n_sink) {
   return p <= qp && (window == 0 || (uint32_t)qp - (uint32_t)p < (uint32_t)window || p < n_sink);
 }
 
+// A product that is rounded before anything is taken from it.
+__device__ __forceinline__ float product(float x, float y) {
+#pragma clang fp contract(off)
+  return x * y;
+}
+
+// Weights are exp2(fma(x, sl2, -ref)), with ref the rounded product of the row's
+// largest x: the fused difference keeps what ref was rounded by, which for a ref of
+// 2^30 is up to 2^6 (weights of 2^64, or a sum of 0).  From this size on (a quarter
+// of a log2 unit) the products are rounded first, so that the largest is ref itself.
+constexpr float kLargeRef = 1 << 22;
+__device__ __forceinline__ bool any_large(float ref) {
+  return __ballot(ref != -INFINITY && fabsf(ref) >= kLargeRef) != 0ull;
+}
+
 template <bool F16>
 __device__ __forceinline__ float elem(uint32_t bits) {
   if constexpr (F16) return (float)__builtin_bit_cast(_Float16, (uint16_t)bits);

@@ -401,6 +401,7 @@ __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, Sp
     float m = -INFINITY, l = 0.f;
 #pragma unroll
     for (int db = 0; db < DB; ++db) o[db] = zero16();
+    bool large = false;           // a row's m is: see kLargeRef
     bool hidden = false;          // some tile held tokens that not all rows see
 
     auto open = [&](int k) {
@@ -564,8 +565,18 @@ __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, Sp
 #pragma unroll
           for (int db = 0; db < DB; ++db) o[db] *= al;
           m = nm;
+          large = any_large(m);
         }
-        const float ref = (m == -INFINITY ? 0.f : m) - kWeightLog<F16>;
+        float ref = m == -INFINITY ? 0.f : m, mul = sl2;
+        if (__builtin_expect(large, 0)) {
+#pragma unroll
+          for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) x[tb][r] = product(x[tb][r], sl2) - ref;
+          ref = 0.f;
+          mul = 1.f;
+        }
+        ref -= kWeightLog<F16>;
         u32x4 ph[4];
         float lt = 0.f;       // the tile's sum: small weights add up before they meet a large l
         {
@@ -584,8 +595,8 @@ __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, Sp
 #pragma unroll
             for (int q = j * 16 / (2 * KS); q < (j + 1) * 16 / (2 * KS); ++q) {
               const int tb = q / 8, r = 2 * (q % 8);
-              const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[tb][r], sl2, -ref));
-              const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[tb][r + 1], sl2, -ref));
+              const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[tb][r], mul, -ref));
+              const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[tb][r + 1], mul, -ref));
               lt = q ? lt + (p0 + p1) : p0 + p1;
               ph[q / 4][q % 4] = pack2<F16>(p0, p1);
             }
@@ -749,7 +760,7 @@ __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, Sp
 #pragma unroll
             for (int j = 0; j < 8; ++j) x = fmaf(elem<F16>(chunk_elem(kk, j)), elem<F16>(chunk_elem(qf[ks], j)), x);
           }
-          x = sum32(x) * b.sl2;
+          x = product(sum32(x), b.sl2);
           if (!(t < pt.row_hi && (t >= pt.row_lo || t < pt.rg.n_first))) continue;
           const float nm = fmaxf(m, x), ref = nm == -INFINITY ? 0.f : nm;
           const float al = __builtin_amdgcn_exp2f(m - ref), p = __builtin_amdgcn_exp2f(x - ref);
