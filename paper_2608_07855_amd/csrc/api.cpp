@@ -1751,7 +1751,8 @@ size_t span_bytes(int64_t n0, int64_t st0, int64_t n1, int64_t st1, int64_t d) {
 }
 
 int check_batch(ckv_ctx* c, const ckv_batch_view* kv, const char* what) {
-  if (!kv || !kv->k || !kv->v || !kv->n_tokens)
+  // (without sequences there are no counts, without tokens no keys: empty tensors have no address)
+  if (!kv || (kv->n_seq && (!kv->n_tokens || (kv->max_tokens && (!kv->k || !kv->v)))))
     return fail(c, CKV_ERR_ARG, "%s: the view or one of its pointers is NULL", what);
   if (kv->dtype != CKV_BF16 && kv->dtype != CKV_F16) return fail(c, CKV_ERR_ARG, "%s: unknown dtype %d", what, kv->dtype);
   if (kv->head_dim != 64 && kv->head_dim != 128)
