@@ -55,7 +55,7 @@ def _cut(lens, rows, group, hkv, prefix):
     for n, r in zip(lens, rows):
         k = -(-r * group // 256)
         see = [prefix + min(max(n - r + min(r, step), 1) + i * step, n) for i in range(k)]
-        work, most, blocks = work + sum(see), max([most] + [prefix + n] * (k > 0)), blocks + k
+        work, most, blocks = work + sum(see), max([most] + [prefix + n] * int(k > 0)), blocks + k
     W = 256 // hkv
     return -(-blocks // W) * most > work / W + 6 * 64
 
@@ -76,6 +76,18 @@ def test_many_rows_in_shares(ckv, n, prefix, d):
     got = b.run(P, ctx, b.device(P))
     assert ctx.workspace_bytes() > 0
     check(b, got, b.want(), f"{n} sequences")
+
+
+# --------------------------------------------------------------- many heads
+
+@pytest.mark.parametrize("hq,hkv,lens,rows", [(300, 1, [400, 3], [20, 1]), (300, 1, [2500, 40], [1, 1]),
+                                              (300, 300, [5000, 9], [1, 1]), (520, 260, [150, 30], [70, 2])])
+@pytest.mark.parametrize("prefix", [0, 70])
+def test_many_heads(ckv, hq, hkv, lens, rows, prefix):
+    """Groups of more query heads than a block has rows, and more KV heads than workgroups at a time."""
+    P, ctx = ckv
+    b = Batch(hq + hkv, lens, rows, hq, hkv, 64, prefix=prefix)
+    check(b, b.run(P, ctx, b.device(P)), b.want(), f"{hq} heads on {hkv}")
 
 
 # ---------------------------------------------------------------- far rows
@@ -116,6 +128,45 @@ def test_far_rows(ckv, pool, tok_stride, paged, rows):
     if paged:
         own = view(*(x[1].transpose(0, 1)[None].contiguous().cuda() for x in (b.k, b.v)), 1)
         same(P.ckv_attend_shared(ctx, far, own, q, want=("o", "lse")), torch.cat(b.k), torch.cat(b.v), 0, "shared")
+
+
+# ------------------------------------------------------- hidden shared tokens
+
+@pytest.mark.parametrize("limited", [False, True])
+@pytest.mark.parametrize("rows", [1, 60])
+@pytest.mark.parametrize("type", ["bf16", "fp16"])
+def test_hidden_shared_tokens_hold_anything(ckv, type, rows, limited):
+    """Rows at positions inside the prefix, behind which it holds what is not finite, as the sequences' own tokens do;
+    then one row that sees the first of it, in the block of rows that do not."""
+    P, ctx = ckv
+    if limited:
+        ctx.set_workspace_limit(4096)
+    qpos = [np.arange(rows) + 100 - rows, [40], [99] * rows]
+    b = Batch(40, [rows, 5, 70], [rows, 1, rows], 8, 2, 64, type, prefix=300, qpos=qpos)
+    want = b.want()
+    bad = torch.tensor([float("nan"), float("inf"), -float("inf"), 1.0]).repeat(16).to(TYPES[type])
+
+    def device():
+        """The batch's views with the hidden tokens overwritten; the host (of whose values the tolerances are) stays."""
+        hidden = [b.pk[100:], b.pv[100:]] + b.k + b.v
+        keep = [x.clone() for x in hidden]
+        for x in hidden:
+            x[:] = bad
+        v = b.device(P)
+        for x, y in zip(hidden, keep):
+            x[:] = y
+        return v
+    check(b, b.run(P, ctx, device()), want, "none sees it")
+    b.given_qpos[1] = [100]
+    v = device()
+    o, lse = torch.zeros((2 * rows + 1, 8, 64), dtype=TYPES[type], device="cuda"), torch.zeros((2 * rows + 1, 8), device="cuda")
+    P.ckv_attend_shared(ctx, v["prefix"], v["kv"], v["q"], o=o, lse=lse)
+    with pytest.raises(P.CKVError, match="NONFINITE"):
+        ctx.sync()
+    got = o.cpu().double().numpy(), lse.cpu().double().numpy()
+    assert not np.isfinite(got[0][rows]).any()
+    rest = np.arange(2 * rows + 1) != rows
+    check(b, tuple(x[rest] for x in got), tuple(x[rest] for x in want), "one sees it")
 
 
 # ------------------------------------------------------------- what few rows keep
