@@ -542,7 +542,8 @@ int ckv_select_and_compact(ckv_ctx* ctx, const ckv_cache_view* in,
  * pos[s*pos_stride + t] is the token's absolute position, >= 0 and strictly
  * ascending in t (with another order the calls stay in bounds, and which tokens a row
  * sees is undefined).  NULL: token t is at position t, or, in
- * ckv_attend_shared, at position t behind the shared tokens.  Without sequences
+ * ckv_attend_shared behind n shared tokens, at n + t, whatever positions these
+ * are given: behind a prefix with gaps, kv needs positions of its own.  Without sequences
  * (n_seq 0) every pointer may be NULL, with max_tokens 0 k and v may be. */
 typedef struct ckv_batch_view {
   const uint16_t* k;

@@ -236,8 +236,9 @@ def batch_view(k, v, n_tokens, *, slot=None, pos=None, max_tokens: int | None = 
     Contiguous: k, v [n_seq, Hkv, capacity, d].  Paged (``slot`` int32 [n_seq,
     stride]): k, v [Hkv, pool_rows, d], and token t of sequence s lives in row
     slot[s, t].  n_tokens: int32 [n_seq] (device); pos: int32 [n_seq, stride]
-    or None (token t at position t); max_tokens: the most tokens a sequence
-    may have (default: as many as the tables or the storage hold)."""
+    or None (token t at position t; behind a shared prefix of n tokens at n + t,
+    whatever positions these have); max_tokens: the most tokens a sequence may
+    have (default: as many as the tables or the storage hold)."""
     nd = 4 if slot is None else 3
     if k.dtype not in _DTYPES:
         raise ValueError("k: expected bfloat16 or float16")

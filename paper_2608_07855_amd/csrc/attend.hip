@@ -45,8 +45,8 @@ __device__ __forceinline__ float sum_rows16(float v) {
 // its own two buffers of 32 tokens of K and V (128 KB of LDS a compute unit),
 // filled by direct loads, without any barrier between waves; slots and positions of the tile after the next
 // travel the same way (one load of 32 words each).  64 sequences with windows of
-// 4096 tokens take 200 us (5.3 TB/s), two of 131072 tokens 191 (5.6; a 2 GiB copy
-// reaches 4.8).
+// 4096 tokens take 201 us (5.3 TB/s), two of 131072 tokens 192 (5.6; plain reads of
+// 4 GiB reach 7.1, a 2 GiB copy 4.9).
 //
 // LDS: token r of a tile is row 4 (r % 8) + r / 8, so that a lane of load i
 // (rows i, 8 + i, 16 + i, 24 + i) finds its slots in consecutive words.  The
@@ -426,9 +426,11 @@ AttendPlan plan_narrow(const AttendArgs& a, int64_t max_tokens, bool room) {
   // A workgroup takes 17 us for 1000 tokens, and joining splits costs 5-7 us.
   // Four workgroups a block or more: short splits (one token of a 2048-token
   // cache 12 us, whole 27; of 4 caches of 4096 tokens 19, with splits of 2048
-  // 31).  Fewer: what halves save the join takes (16 caches, a window of 1024
-  // tokens: whole 14.7, in halves 16.2 us).
-  // (Of `blocks` about two thirds are there.)
+  // 31).  Fewer: what halves save the join takes (16 caches with about 500 tokens
+  // in the window: whole 14.7, in halves 16.2 us).
+  // (Of `blocks` about two thirds are there, so 10 sequences of 8 KV heads, 80
+  // blocks, count as more than 96: 10 caches of 2000 tokens take 28.5 us whole, of
+  // 2100 tokens in two splits 24.3, and 8 of 2000 in eight 19.1.)
   const bool small = blocks * a.Hkv <= 96;
   const int64_t seen = a.window ? std::min(max_tokens, (int64_t)a.window + a.n_sink + a.max_rows) : max_tokens;
   p.min_chunk = small ? 256 : 2048;

@@ -29,13 +29,20 @@ namespace {
 // 2^-38 of it at most).  A lag of 8 would leave 2^-21 and saves 1% at best (16
 // fp16 chunks behind a 16K prefix 760, with a lag of 4 763, of 2 769 us).
 //
+// Weights are rounded once to the type before they multiply the values (float32
+// in the sums).  o's error against 64 bits then grows from its own rounding's
+// 0.0017 of o to 0.0019 (prompts, a 64K prefix) or 0.0022 (the largest drawn) in bf16,
+// and from 0.00021 to 0.00022 in fp16.  A second product for the rest of each
+// weight, as few rows have it, takes that away and 22% (a prompt of 4096 tokens 256
+// -> 313 us) to 32% longer (the 64K prefix's call 632 -> 836), and spills.
+//
 // Bound: matrix and vector issue.  A step is 32 products (1024 cycles) and about
-// 140 vector instructions a wave; both waves of a SIMD pass the same barrier a
+// 150 vector instructions a wave; both waves of a SIMD pass the same barrier a
 // tile, so each interleaves the two for itself (see step()): 256 rows of 64
-// heads on 65536 shared tokens take 572 us, 0.96 PFLOP/s, 16 chunks behind a 16K
-// prefix 775 us, 0.76 (an 8192^3 product reaches 1.2), the matrix units busy 45%
-// and the vector units 50% of the cycles at 1.8 to 2.1 GHz.  (64 rows a wave and
-// one wave a SIMD read LDS half as often, but spill.)
+// heads on 65536 shared tokens take 540 us, 1.0 PFLOP/s (588 from an idle device),
+// the matrix units busy 46% and the vector units 45% of the cycles, 16 fp16 chunks
+// behind a 16K prefix 765 us, 0.77 (37% and 40%; an 8192^3 product reaches 1.2).
+// (64 rows a wave and one wave a SIMD read LDS half as often, but spill.)
 //
 // Work is cut evenly: workgroup e of a KV head takes the same share of the
 // head's tokens-to-see as every other, wherever that begins and ends; a block

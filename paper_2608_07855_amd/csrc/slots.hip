@@ -17,8 +17,10 @@
 // store (1024 prompts, 920K tokens, 13.5 us; a thread per token spent its time
 // finding each token's sequence: 16.6).
 //
-// Bound: latency.  A step reads two counts a sequence, moves two words a
-// block and writes four words a token.
+// Bound: latency (a decoding step of 64 sequences 5.4 us), and with many new
+// tokens the stores: a step reads two counts a sequence, moves two words a block
+// and writes four words a token, a lane's run of 64 bytes apart from its
+// neighbour's in each of four arrays (most of what the 13.5 us above have over the 5.4).
 #include "ckv_device.h"
 #include "ckv_kernels.h"
 
