@@ -231,6 +231,14 @@ def _check_flat(t, name, n, device=None):
         raise ValueError(f"{name}: expected a contiguous tensor of {n} entries")
 
 
+def _int32(x, name):
+    """x as an int that the C struct holds (a larger one would lose its upper bits there, without a word)."""
+    x = int(x)
+    if not -2**31 <= x < 2**31:
+        raise ValueError(f"{name} {x} does not fit 32 bits")
+    return x
+
+
 def batch_view(k, v, n_tokens, *, slot=None, pos=None, max_tokens: int | None = None) -> BatchView:
     """Caches of several sequences of one layer, bf16 or fp16.
     Contiguous: k, v [n_seq, Hkv, capacity, d].  Paged (``slot`` int32 [n_seq,
@@ -291,7 +299,7 @@ def query_view(q, cu_rows, qpos=None, *, max_rows: int | None = None, scale: flo
         raise ValueError("cu_rows holds n_seq + 1 entries")
     if qpos is not None:
         _check_flat(qpos, "qpos", q.shape[0], q.device)
-    most = max(1, -(-q.shape[0] // max(n, 1))) if max_rows is None else int(max_rows)
+    most = max(1, -(-q.shape[0] // max(n, 1))) if max_rows is None else _int32(max_rows, "max_rows")
     view = QueryView(q.data_ptr(), q.stride(0), q.stride(1), cu_rows.data_ptr(),
                      None if qpos is None else qpos.data_ptr(), q.shape[1], q.shape[0], most, float(scale))
     view._keep = (q, cu_rows, qpos)
@@ -306,7 +314,7 @@ def slot_step(n_tokens, n_new, free, n_free, slot, *, block_size: int, block_tab
     [n_blocks], a stack of which n_free [1] entries are free; slot, pos
     [n_seq, stride]; block_table [n_seq, stride] (may be None with block_size
     1).  Outputs are allocated here unless given; new_row and new_pos hold
-    max_new entries (default: as many as the tables could take)."""
+    max_new entries (default: as many as the tables could take, below 2^31)."""
     n, dev = n_tokens.numel(), n_tokens.device
     _check_flat(n_tokens, "n_tokens", n)
     _check_flat(n_new, "n_new", n, dev)
@@ -322,7 +330,8 @@ def slot_step(n_tokens, n_new, free, n_free, slot, *, block_size: int, block_tab
     if next_pos is not None:
         _check_flat(next_pos, "next_pos", n, dev)
     if max_new is None:
-        max_new = new_row.numel() if new_row is not None else n * slot.shape[1]
+        max_new = min(new_row.numel() if new_row is not None else n * slot.shape[1], 2**31 - 1)
+    max_new = _int32(max_new, "max_new")
 
     def out(t, name, m):
         if t is None:
@@ -338,7 +347,7 @@ def slot_step(n_tokens, n_new, free, n_free, slot, *, block_size: int, block_tab
 
     def rows(t):
         return (0, 0) if t is None else (t.stride(0), t.shape[1])
-    step = SlotStep(n, int(block_size), free.numel(), int(max_new), p(n_tokens), p(n_new), p(next_pos), p(n_free),
+    step = SlotStep(n, _int32(block_size, "block_size"), free.numel(), max_new, p(n_tokens), p(n_new), p(next_pos), p(n_free),
                     p(free), p(block_table), *rows(block_table), p(slot), p(pos), *rows(slot), p(n_tokens_out),
                     p(n_free_out), p(cu_new), p(new_row), p(new_pos), p(status))
     step._keep = (n_tokens, n_new, next_pos, n_free, free, block_table, slot, pos)
@@ -570,8 +579,8 @@ def ckv_attend_window(ctx: Context, kv: BatchView, q: QueryView, *, window: int 
     to p).  o [n_rows, Hq, d] of the queries' type; "lse" in ``want`` (or a
     given ``lse``): float32 [n_rows, Hq]."""
     o, lse = _attend_outputs(ctx, (kv,), q, o, lse, want)
-    ctx.check(ctx._lib.ckv_attend_window(ctx.handle, ctypes.byref(kv), ctypes.byref(q), int(window), int(n_sink),
-                                         o.data_ptr(), None if lse is None else lse.data_ptr()))
+    ctx.check(ctx._lib.ckv_attend_window(ctx.handle, ctypes.byref(kv), ctypes.byref(q), _int32(window, "window"),
+                                         _int32(n_sink, "n_sink"), o.data_ptr(), None if lse is None else lse.data_ptr()))
     return dict(o=o, lse=lse)
 
 
