@@ -28,6 +28,10 @@
  *                             window and first tokens that stay visible.
  *   ckv_attend_shared         attention of a batch whose sequences begin with
  *                             the same tokens, read once for all.
+ *   ckv_pack_tokens           new tokens' keys and values written into a pool
+ *                             that holds them in 4 bits.
+ *   ckv_unpack_tokens         such caches read back into 16 bits.
+ *   ckv_attend_packed         ckv_attend_window over such caches.
  *
  * Conventions shared by every call
  * --------------------------------
@@ -712,6 +716,115 @@ typedef struct ckv_slot_step {
  * rows alternate in one buffer overlap).
  */
 int ckv_build_slots(ckv_ctx* ctx, const ckv_slot_step* step);
+
+/* ------------------------------------------------------- caches in 4 bits */
+
+/* A packed row holds the key and the value of ONE token of ONE KV head in 4 bits
+ * a width, CKV_PACKED_ROW_BYTES(d) bytes (d = head_dim):
+ *   [0, d/2)           codes of the key
+ *   [d/2, d)           codes of the value
+ *   [d, d + d/8)       for each group of 32 widths of the key a scale s and a base
+ *                      b, two fp16 numbers
+ *   [d + d/8, 5d/4)    the same of the value
+ * Code n (0 to 15) of a group stands for s * (16 + n) + b, rounded once to fp16.
+ * 32-bit word j of a key's (value's) codes holds widths 8j to 8j+7: width 8j + 2p
+ * in bits 4p to 4p+3 and width 8j + 2p + 1 in bits 16+4p to 19+4p, p = 0..3. */
+#define CKV_PACKED_ROW_BYTES(d) ((d) / 4 * 5)
+
+/* Rows of a pool of packed rows: row r of KV head g begins at data +
+ * g*head_stride + r*row_stride.  Strides in bytes, multiples of 16; data is 16-byte
+ * aligned. */
+typedef struct ckv_packed_pool {
+  uint8_t* data;
+  int64_t head_stride;
+  int64_t row_stride;        /* CKV_PACKED_ROW_BYTES(head_dim) or more */
+  int32_t pool_rows;
+  int32_t n_kv_heads;
+  int32_t head_dim;          /* 64 or 128 */
+} ckv_packed_pool;
+
+/* Keys and values in 16 bits: of token t (of sequence s, where there are
+ * several) and head g at s*seq_stride + g*head_stride + t*tok_stride (elements,
+ * multiples of 8; rows 16-byte aligned). */
+typedef struct ckv_kv_rows {
+  uint16_t* k;
+  uint16_t* v;
+  int64_t seq_stride;
+  int64_t head_stride;
+  int64_t tok_stride;
+  int32_t dtype;             /* CKV_BF16 or CKV_F16 */
+} ckv_kv_rows;
+
+/* Packed caches of ONE layer of n_seq sequences, as ckv_batch_view describes
+ * caches in 16 bits: token t of sequence s is row t of data + s*seq_stride, or,
+ * with `slot`, row slot[s*slot_stride + t] of a pool that all sequences share
+ * (values outside [0, pool_rows) are clamped to the last row).  Strides in
+ * bytes, multiples of 16.  n_tokens, pos, max_tokens as there. */
+typedef struct ckv_packed_view {
+  const uint8_t* data;
+  int64_t seq_stride;        /* ignored with slot */
+  int64_t head_stride;
+  int64_t row_stride;
+  const int32_t* slot;       /* device int32, or NULL: contiguous */
+  int64_t slot_stride;
+  const int32_t* pos;        /* device int32, or NULL */
+  int64_t pos_stride;
+  const int32_t* n_tokens;   /* device int32[n_seq] */
+  int32_t n_seq;
+  int32_t max_tokens;
+  int32_t pool_rows;         /* with slot */
+  int32_t n_kv_heads;
+  int32_t head_dim;          /* 64 or 128 */
+} ckv_packed_view;
+
+/*
+ * Quantises n_rows tokens (in->seq_stride is ignored) and writes token t of every
+ * KV head into row row[t] of the pool (device int32[n_rows], such as
+ * ckv_slot_step's new_row).  Tokens from *n_live on (device int32[1], clamped to
+ * [0, n_rows]; NULL: n_rows, such as the last entry of cu_new) and tokens whose row lies
+ * outside [0, pool_rows) write nothing, so a captured step serves any number of
+ * tokens.  Rows of one call must differ; of tokens that share one, its groups
+ * hold either's.
+ *
+ * For a group of 32 widths with smallest element m and largest M (elements
+ * clamped to [-16384, 16384]), in float32:
+ *   s = fp16((M - m) / 15),  b = fp16(m - 16 s) (a zero is +0),  t = x - b,
+ *   n = the largest of 1..15 with t >= (15.5 + n) s, or 0,
+ * that is the code whose value lies nearest (ties up).  A value differs from its
+ * element by s/2 at most, and by what rounding s, b and the value to fp16 adds.
+ * A group that holds a NaN or an infinity gets s = 0 and b = NaN: all of it reads
+ * back as NaN, and an attention that sees it reports CKV_ERR_NONFINITE.
+ * Errors: CKV_ERR_ARG (NULL pointers, alignment, an unknown type, the pool
+ * overlapping the input), CKV_ERR_SHAPE (widths, heads, strides, sizes).
+ */
+int ckv_pack_tokens(ckv_ctx* ctx, const ckv_kv_rows* in, const int32_t* row,
+                    int32_t n_rows, const int32_t* n_live,
+                    const ckv_packed_pool* pool);
+
+/*
+ * Reads packed caches back: the keys and values that token t < n_tokens[s] of
+ * sequence s stands for, rounded once more to out->dtype, go to `out` (for
+ * ckv_measure_page_effects, ckv_select_and_compact and whatever else takes 16
+ * bits).  Rows from n_tokens[s] on are left as they were; out holds max_tokens
+ * rows of each sequence and head, none of which may lie on another (its
+ * strides as ckv_kv_rows).  Positions play no part.
+ * Errors: as ckv_pack_tokens; CKV_ERR_ARG where out overlaps the caches.
+ */
+int ckv_unpack_tokens(ckv_ctx* ctx, const ckv_packed_view* kv,
+                      const ckv_kv_rows* out);
+
+/*
+ * ckv_attend_window over packed caches.  dtype: of queries and outputs.  Keys and
+ * values are the fp16 numbers that the codes stand for; which tokens a row sees,
+ * outputs, hidden tokens, workspace, capture and errors are as there.
+ * Precision: bf16 queries are taken as fp16 times a power of two of each row's own
+ * (elements below 2^-29 of the row's largest lose bits, 2^-40 of it at most), softmax
+ * weights are rounded once to fp16 as there (for fp16 outputs of few rows: weight
+ * and rest); float32 logits, maxima, sums and accumulation.
+ */
+int ckv_attend_packed(ckv_ctx* ctx, const ckv_packed_view* kv,
+                      const ckv_query_view* q, int32_t dtype, int32_t window,
+                      int32_t n_sink, void* o, float* lse);
 
 #ifdef __cplusplus
 }

@@ -115,6 +115,24 @@ class SlotStep(ctypes.Structure):
                 ("new_pos", ctypes.c_void_p), ("status", ctypes.c_void_p)]
 
 
+class PackedPool(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("head_stride", ctypes.c_int64), ("row_stride", ctypes.c_int64),
+                ("pool_rows", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
+
+
+class KVRows(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("seq_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64), ("tok_stride", ctypes.c_int64), ("dtype", ctypes.c_int32)]
+
+
+class PackedView(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("seq_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("row_stride", ctypes.c_int64), ("slot", ctypes.c_void_p), ("slot_stride", ctypes.c_int64),
+                ("pos", ctypes.c_void_p), ("pos_stride", ctypes.c_int64), ("n_tokens", ctypes.c_void_p),
+                ("n_seq", ctypes.c_int32), ("max_tokens", ctypes.c_int32), ("pool_rows", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
+
+
 POOL_MAX, POOL_MEAN = 0, 1
 BF16, F16 = 0, 1
 SLOTS_OK, SLOTS_NO_BLOCKS, SLOTS_TABLE, SLOTS_MAX_NEW, SLOTS_BAD_COUNT = range(5)
@@ -203,6 +221,13 @@ SIGNATURES = {
         ctypes.c_void_p, ctypes.POINTER(BatchView), ctypes.POINTER(BatchView), ctypes.POINTER(QueryView),
         ctypes.c_void_p, ctypes.c_void_p]),
     "ckv_build_slots": (ctypes.c_int, [ctypes.c_void_p, ctypes.POINTER(SlotStep)]),
+    "ckv_pack_tokens": (ctypes.c_int, [
+        ctypes.c_void_p, ctypes.POINTER(KVRows), ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p,
+        ctypes.POINTER(PackedPool)]),
+    "ckv_unpack_tokens": (ctypes.c_int, [ctypes.c_void_p, ctypes.POINTER(PackedView), ctypes.POINTER(KVRows)]),
+    "ckv_attend_packed": (ctypes.c_int, [
+        ctypes.c_void_p, ctypes.POINTER(PackedView), ctypes.POINTER(QueryView), ctypes.c_int32, ctypes.c_int32,
+        ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p]),
     "ckv_agent_create": (ctypes.c_int, [ctypes.c_void_p, ctypes.POINTER(CacheView),
                                         ctypes.POINTER(CacheView), ctypes.POINTER(AgentConfig),
                                         ctypes.POINTER(ctypes.c_void_p)]),

@@ -15,8 +15,8 @@ import numpy as np
 import torch
 
 from . import _abi
-from ._abi import (AcceptedPages, BatchView, Budget, CacheView, KVView, PageList, QueryView, SlotStep, Thresholds,
-                   WindowView)
+from ._abi import (AcceptedPages, BatchView, Budget, CacheView, KVRows, KVView, PackedPool, PackedView, PageList,
+                   QueryView, SlotStep, Thresholds, WindowView)
 
 PAPER_THRESHOLDS = dict(tau_use=0.05, tau_dead=0.01, rho_use=0.75, rho_dead=0.25, tau_joint=0.01)
 
@@ -281,6 +281,52 @@ def batch_view(k, v, n_tokens, *, slot=None, pos=None, max_tokens: int | None = 
                      _DTYPES[k.dtype])
     view._keep = (k, v, n_tokens, slot, pos)   # the struct holds raw pointers: keep the tensors alive
     view._device, view._torch_dtype = k.device, k.dtype
+    return view
+
+
+def packed_row_bytes(head_dim: int) -> int:
+    """Bytes of a packed row: key and value of one token of one KV head in 4 bits."""
+    return head_dim // 4 * 5
+
+
+def _check_packed(pool, name, ndim):
+    _check_dev(pool, name, torch.uint8, ndim)
+    if pool.shape[-1] not in (packed_row_bytes(64), packed_row_bytes(128)):
+        raise ValueError(f"{name}: rows of {pool.shape[-1]} bytes; a packed row has {packed_row_bytes(64)} or {packed_row_bytes(128)}")
+
+
+def packed_view(pool, n_tokens, *, slot=None, pos=None, max_tokens: int | None = None) -> PackedView:
+    """Caches of several sequences of one layer in 4 bits (uint8).  Contiguous:
+    pool [n_seq, Hkv, capacity, packed_row_bytes(d)].  Paged (``slot`` int32
+    [n_seq, stride]): pool [Hkv, pool_rows, packed_row_bytes(d)], and token t of
+    sequence s lives in row slot[s, t].  n_tokens, pos, max_tokens as in batch_view."""
+    _check_packed(pool, "pool", 4 if slot is None else 3)
+    n = n_tokens.numel()
+    _check_flat(n_tokens, "n_tokens", n, pool.device)
+    if slot is None:
+        if pool.shape[0] != n:
+            raise ValueError(f"pool holds {pool.shape[0]} sequences, n_tokens {n}")
+        room = pool.shape[2]
+    else:
+        _check_dev(slot, "slot", torch.int32, 2, pool.device)
+        if slot.shape[0] != n:
+            raise ValueError(f"slot holds {slot.shape[0]} sequences, n_tokens {n}")
+        room = slot.shape[1]
+    if pos is not None:
+        _check_dev(pos, "pos", torch.int32, 2, pool.device)
+        if pos.shape[0] != n:
+            raise ValueError(f"pos holds {pos.shape[0]} sequences, n_tokens {n}")
+        room = min(room, pos.shape[1])
+    most = room if max_tokens is None else int(max_tokens)
+    if not 0 <= most <= room:
+        raise ValueError(f"max_tokens {most} out of range (the tables hold {room})")
+    st = pool.stride()
+    view = PackedView(pool.data_ptr(), st[0] if slot is None else 0, st[-3], st[-2],
+                      None if slot is None else slot.data_ptr(), 0 if slot is None else slot.stride(0),
+                      None if pos is None else pos.data_ptr(), 0 if pos is None else pos.stride(0), n_tokens.data_ptr(), n,
+                      most, 0 if slot is None else pool.shape[-2], pool.shape[-3], pool.shape[-1] // 5 * 4)
+    view._keep = (pool, n_tokens, slot, pos)   # the struct holds raw pointers: keep the tensors alive
+    view._device = pool.device
     return view
 
 
@@ -552,7 +598,7 @@ def ckv_select_and_compact(ctx: Context, k_in, v_in, pos_in, n_tokens, score, re
 
 def _attend_outputs(ctx, views, q, o, lse, want):
     for x in views:
-        if x._torch_dtype != q._torch_dtype or x._device != q._device:
+        if getattr(x, "_torch_dtype", q._torch_dtype) != q._torch_dtype or x._device != q._device:
             raise ValueError("caches and queries must agree in type and device")
     if q._device.index != ctx.device:
         raise ValueError(f"the tensors are on {q._device}, the context on device {ctx.device}")
@@ -604,6 +650,66 @@ def ckv_build_slots(ctx: Context, step: SlotStep):
         raise ValueError(f"the tables are on {step._device}, the context on device {ctx.device}")
     ctx.check(ctx._lib.ckv_build_slots(ctx.handle, ctypes.byref(step)))
     return step._out
+
+
+def _check_rows_16(ctx, k, v, ndim, pool_device):
+    if k.dtype not in _DTYPES:
+        raise ValueError("k: expected bfloat16 or float16")
+    _check_dev(k, "k", k.dtype, ndim, pool_device)
+    _check_dev(v, "v", k.dtype, ndim, pool_device)
+    if k.shape != v.shape or k.stride() != v.stride():
+        raise ValueError("k and v must have the same shape and strides")
+    if pool_device.index != ctx.device:
+        raise ValueError(f"the tensors are on {pool_device}, the context on device {ctx.device}")
+
+
+def ckv_pack_tokens(ctx: Context, k, v, row, pool, *, n_live=None):
+    """Quantises the keys and values k, v [n, Hkv, d] (bf16 or fp16, alike in strides) of n
+    tokens to 4 bits, token t into row row[t] (int32 [n]) of every head of pool
+    (uint8 [Hkv, pool_rows, packed_row_bytes(d)]).  Tokens from n_live[0] on (int32 [1], device;
+    None: all live) and tokens whose row lies outside the pool are left out; the rows of
+    the others must differ."""
+    _check_packed(pool, "pool", 3)
+    _check_rows_16(ctx, k, v, 3, pool.device)
+    n, hkv, d = k.shape
+    if hkv != pool.shape[0] or packed_row_bytes(d) != pool.shape[2]:
+        raise ValueError(f"the pool has {pool.shape[0]} heads and rows of {pool.shape[2]} bytes, the tokens {hkv} and "
+                         f"{packed_row_bytes(d)}")
+    _check_flat(row, "row", n, pool.device)
+    if n_live is not None:
+        _check_flat(n_live, "n_live", 1, pool.device)
+    rows = KVRows(k.data_ptr(), v.data_ptr(), 0, k.stride(1), k.stride(0), _DTYPES[k.dtype])
+    to = PackedPool(pool.data_ptr(), pool.stride(0), pool.stride(1), pool.shape[1], hkv, d)
+    ctx.check(ctx._lib.ckv_pack_tokens(ctx.handle, ctypes.byref(rows), row.data_ptr(), _int32(n, "n"),
+                                       None if n_live is None else n_live.data_ptr(), ctypes.byref(to)))
+    return pool
+
+
+def ckv_unpack_tokens(ctx: Context, kv: PackedView, *, k=None, v=None, dtype=torch.bfloat16):
+    """The keys and values that packed caches stand for: k, v [n_seq, Hkv, max_tokens, d]
+    (or more tokens) of ``dtype``, unless given.  Rows past a sequence's tokens keep what they held
+    (zeros where they are allocated here)."""
+    shape = (kv.n_seq, kv.n_kv_heads, kv.max_tokens, kv.head_dim)
+    if (k is None) != (v is None):
+        raise ValueError("k and v are given both or not at all")
+    if k is None:
+        k, v = (torch.zeros(shape, dtype=dtype, device=kv._device) for _ in range(2))
+    _check_rows_16(ctx, k, v, 4, kv._device)
+    if (k.shape[0], k.shape[1], k.shape[3]) != (shape[0], shape[1], shape[3]) or k.shape[2] < shape[2]:
+        raise ValueError(f"k and v: expected {shape} or more tokens, not {tuple(k.shape)}")
+    out = KVRows(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2), _DTYPES[k.dtype])
+    ctx.check(ctx._lib.ckv_unpack_tokens(ctx.handle, ctypes.byref(kv), ctypes.byref(out)))
+    return dict(k=k, v=v)
+
+
+def ckv_attend_packed(ctx: Context, kv: PackedView, q: QueryView, *, window: int = 0, n_sink: int = 0, o=None, lse=None,
+                      want=("o",)):
+    """ckv_attend_window over packed caches; o is of the queries' type."""
+    o, lse = _attend_outputs(ctx, (kv,), q, o, lse, want)
+    ctx.check(ctx._lib.ckv_attend_packed(ctx.handle, ctypes.byref(kv), ctypes.byref(q), _DTYPES[q._torch_dtype],
+                                         _int32(window, "window"), _int32(n_sink, "n_sink"), o.data_ptr(),
+                                         None if lse is None else lse.data_ptr()))
+    return dict(o=o, lse=lse)
 
 
 # ---------------------------------------------------------------- lifecycle driver

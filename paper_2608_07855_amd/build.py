@@ -28,7 +28,7 @@ BUILD_DIR = os.path.join(PKG, "_build")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 SOURCES = ["api.cpp", "agent.cpp", "measure.hip", "recorded.hip", "classify.hip", "joint.hip", "select.hip",
-           "attend.hip", "attend_wide.hip", "slots.hip"]
+           "attend.hip", "attend_wide.hip", "attend_packed.hip", "packed.hip", "slots.hip"]
 
 COMMON = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -1772,10 +1772,10 @@ int check_batch(ckv_ctx* c, const ckv_batch_view* kv, const char* what) {
   return CKV_OK;
 }
 
-int check_query(ckv_ctx* c, const ckv_query_view* q, const ckv_batch_view* kv, const void* o, const float* lse) {
+int check_query(ckv_ctx* c, const ckv_query_view* q, int32_t n_kv_heads, int32_t head_dim, const void* o, const float* lse) {
   if (!q || !q->cu_rows) return fail(c, CKV_ERR_ARG, "query view or cu_rows is NULL");
-  if (q->n_q_heads < 1 || q->n_q_heads % kv->n_kv_heads)
-    return fail(c, CKV_ERR_SHAPE, "n_q_heads %d is not a multiple of n_kv_heads %d", q->n_q_heads, kv->n_kv_heads);
+  if (q->n_q_heads < 1 || q->n_q_heads % n_kv_heads)
+    return fail(c, CKV_ERR_SHAPE, "n_q_heads %d is not a multiple of n_kv_heads %d", q->n_q_heads, n_kv_heads);
   if (q->n_rows < 0 || (int64_t)q->n_rows * q->n_q_heads > INT_MAX - 1024)
     return fail(c, CKV_ERR_SHAPE, "n_rows %d out of range", q->n_rows);
   if (q->max_rows < 1) return fail(c, CKV_ERR_SHAPE, "max_rows must be >= 1");
@@ -1785,8 +1785,8 @@ int check_query(ckv_ctx* c, const ckv_query_view* q, const ckv_batch_view* kv, c
   if (!aligned16(q->q) || q->row_stride % 8 || q->head_stride % 8 || !aligned16(o))
     return fail(c, CKV_ERR_ARG, "query and output rows must be 16-byte aligned (strides multiples of 8)");
   if (q->row_stride < 0 || q->head_stride < 0) return fail(c, CKV_ERR_SHAPE, "query strides must not be negative");
-  const size_t nq = span_bytes(q->n_rows, q->row_stride, q->n_q_heads, q->head_stride, kv->head_dim);
-  const size_t rows = (size_t)q->n_rows * q->n_q_heads, no = rows * kv->head_dim * 2, nl = rows * 4;
+  const size_t nq = span_bytes(q->n_rows, q->row_stride, q->n_q_heads, q->head_stride, head_dim);
+  const size_t rows = (size_t)q->n_rows * q->n_q_heads, no = rows * head_dim * 2, nl = rows * 4;
   if (overlap(o, no, q->q, nq) || overlap(lse, nl, q->q, nq) || overlap(o, no, lse, nl))
     return fail(c, CKV_ERR_ARG, "outputs overlap the queries or each other");
   return CKV_OK;
@@ -1831,52 +1831,53 @@ bool take_few(const AttendArgs& a, int64_t n_pre, int64_t n_own) {
   return packed * n_pre + n * std::max(1.0, 0.7 * blocks) * n_own <= n * wide * (double)(n_pre + n_own);
 }
 
-int attend(ckv_ctx* c, const ckv_batch_view* pre, const ckv_batch_view* kv, const ckv_query_view* q, int32_t window,
-           int32_t n_sink, void* o, float* lse) {
-  if (q->n_rows == 0 || kv->n_seq == 0) return CKV_OK;
-  DeviceGuard g(c->device);
-  if (!g.ok) return fail(c, CKV_ERR_HIP, "cannot select device %d", c->device);
-  AttendArgs a;
-  a.own = make_caches(kv);
-  a.pre = make_caches(pre ? pre : kv);
-  a.has_pre = pre != nullptr;
-  a.f16 = kv->dtype == CKV_F16;
+// what the attention calls take from the queries and outputs
+void set_rows(ckv_ctx* c, AttendArgs& a, const ckv_query_view* q, int32_t n_kv_heads, int32_t head_dim, int32_t dtype, int32_t window,
+              int32_t n_sink, void* o, float* lse) {
+  a.f16 = dtype == CKV_F16;
   a.q = q->q;
   a.q_row_stride = q->row_stride;
   a.q_head_stride = q->head_stride;
   a.cu_rows = q->cu_rows;
   a.qpos = q->qpos;
   a.Hq = q->n_q_heads;
-  a.Hkv = kv->n_kv_heads;
+  a.Hkv = n_kv_heads;
   a.group = a.Hq / a.Hkv;
-  a.D = kv->head_dim;
+  a.D = head_dim;
   a.n_rows = q->n_rows;
   a.max_rows = q->max_rows;
   a.window = window;
   a.n_sink = n_sink;
-  const float scale = q->scale > 0.f ? q->scale : 1.0f / std::sqrt((float)kv->head_dim);
+  const float scale = q->scale > 0.f ? q->scale : 1.0f / std::sqrt((float)head_dim);
   a.sl2 = scale * kLog2eHost;
   a.o = static_cast<uint16_t*>(o);
   a.lse = lse;
   a.nonfinite = c->nf_dev;
-  bool few = take_few(a, pre ? pre->max_tokens : 0, kv->max_tokens);
-  AttendPlan p = few ? plan_narrow(a, kv->max_tokens, true) : plan_wide(a, true);
+}
+
+// n_pre, n_own: the host's bounds of the shared and of a sequence's own tokens
+int attend_rows(ckv_ctx* c, const AttendArgs& a, int64_t n_pre, int64_t n_own) {
+  if (a.n_rows == 0 || a.own.n_seq == 0) return CKV_OK;
+  DeviceGuard g(c->device);
+  if (!g.ok) return fail(c, CKV_ERR_HIP, "cannot select device %d", c->device);
+  bool few = a.packed || take_few(a, n_pre, n_own);
+  AttendPlan p = few ? plan_narrow(a, n_own, true) : plan_wide(a, true);
   PrefixPlan pf = {0, 0, 0};
-  if (pre && few) pf = plan_prefix(a);
+  if (a.has_pre && few) pf = plan_prefix(a);
   auto floats = [&](int64_t items, int rows) { return round_up((size_t)items * rows * (a.D + 2) * sizeof(float), kAlign); };
   const int64_t pre_items = pf.blocks * pf.n_split * a.Hkv;
   const size_t pre_bytes = floats(pre_items, pf.rows);
   const size_t own_bytes = !p.split ? 0 : floats(p.items, p.rows) + (few ? 0 : p.items * sizeof(int4));
   bool room = true;
   if (std::max(p.grid, few ? pre_items : 0) > kMostGroups)
-    return fail(c, CKV_ERR_UNSUPPORTED, "%d rows of %d sequences and %d KV heads are more than one call can launch", q->n_rows,
-                kv->n_seq, kv->n_kv_heads);
+    return fail(c, CKV_ERR_UNSUPPORTED, "%d rows of %d sequences and %d KV heads are more than one call can launch", a.n_rows,
+                a.own.n_seq, a.Hkv);
   if (own_bytes + pre_bytes > 0)
     if (int rc = ensure_attend_ws(c, own_bytes + pre_bytes, &room)) return rc;
   if (!room) {
     // without partial sums, the many-rows kernel alone reads two parts in one pass
-    few = few && !pre;
-    p = few ? plan_narrow(a, kv->max_tokens, false) : plan_wide(a, false);
+    few = few && !a.has_pre;
+    p = few ? plan_narrow(a, n_own, false) : plan_wide(a, false);
     if (p.grid > kMostGroups) return fail(c, CKV_ERR_NOMEM, "the workspace limit leaves no room for the call's partial sums");
   }
   auto space = [&](size_t off, int64_t items, int rows) {
@@ -1891,7 +1892,7 @@ int attend(ckv_ctx* c, const ckv_batch_view* pre, const ckv_batch_view* kv, cons
   const SplitSpace own = p.split ? space(pre_bytes, p.items, p.rows) : none;
   if (few) {
     PrefixParts pp = {nullptr, nullptr, 0, 1};
-    if (pre) {
+    if (a.has_pre) {
       const SplitSpace sp = space(0, pre_items, pf.rows);
       pp = {sp.o, sp.ml, pf.n_split, pf.rows};
       CKV_LAUNCH(c, "attend_prefix", launch_attend_prefix(a, pf, sp, c->stream));
@@ -1904,6 +1905,17 @@ int attend(ckv_ctx* c, const ckv_batch_view* pre, const ckv_batch_view* kv, cons
   return CKV_OK;
 }
 
+int attend(ckv_ctx* c, const ckv_batch_view* pre, const ckv_batch_view* kv, const ckv_query_view* q, int32_t window,
+           int32_t n_sink, void* o, float* lse) {
+  AttendArgs a;
+  a.own = make_caches(kv);
+  a.pre = make_caches(pre ? pre : kv);
+  a.has_pre = pre != nullptr;
+  a.packed = false;
+  set_rows(c, a, q, kv->n_kv_heads, kv->head_dim, kv->dtype, window, n_sink, o, lse);
+  return attend_rows(c, a, pre ? pre->max_tokens : 0, kv->max_tokens);
+}
+
 }  // namespace
 
 extern "C" int ckv_attend_window(ckv_ctx* c, const ckv_batch_view* kv, const ckv_query_view* q, int32_t window,
@@ -1913,7 +1925,7 @@ extern "C" int ckv_attend_window(ckv_ctx* c, const ckv_batch_view* kv, const ckv
   begin_call(c);
   if (int rc0 = latched_nonfinite(c)) return rc0;
   int rc;
-  if ((rc = check_batch(c, kv, "caches")) || (rc = check_query(c, q, kv, o, lse))) return rc;
+  if ((rc = check_batch(c, kv, "caches")) || (rc = check_query(c, q, kv->n_kv_heads, kv->head_dim, o, lse))) return rc;
   if (window < 0 || n_sink < 0) return fail(c, CKV_ERR_ARG, "window %d and n_sink %d must not be negative", window, n_sink);
   return attend(c, nullptr, kv, q, window, n_sink, o, lse);
 }
@@ -1925,7 +1937,7 @@ extern "C" int ckv_attend_shared(ckv_ctx* c, const ckv_batch_view* prefix, const
   begin_call(c);
   if (int rc0 = latched_nonfinite(c)) return rc0;
   int rc;
-  if ((rc = check_batch(c, prefix, "prefix")) || (rc = check_batch(c, kv, "caches")) || (rc = check_query(c, q, kv, o, lse)))
+  if ((rc = check_batch(c, prefix, "prefix")) || (rc = check_batch(c, kv, "caches")) || (rc = check_query(c, q, kv->n_kv_heads, kv->head_dim, o, lse)))
     return rc;
   if (prefix->n_seq != 1) return fail(c, CKV_ERR_SHAPE, "prefix: a view of one sequence is expected, not %d", prefix->n_seq);
   if (prefix->dtype != kv->dtype || prefix->head_dim != kv->head_dim || prefix->n_kv_heads != kv->n_kv_heads)
@@ -2000,4 +2012,194 @@ extern "C" int ckv_build_slots(ckv_ctx* c, const ckv_slot_step* st) {
   a.status = st->status;
   CKV_LAUNCH(c, "slots", launch_slots(a, c->stream));
   return CKV_OK;
+}
+
+// ------------------------------------------------------------ caches in 4 bits
+
+namespace {
+
+// n rows of `st` bytes' distance, as far as they can be told apart; INT64_MAX where they pass it
+int64_t extent(int64_t n, int64_t st) { return n <= 1 || st == 0 ? 0 : n - 1 > INT64_MAX / 4 / st ? INT64_MAX / 4 : (n - 1) * st; }
+
+int check_packed(ckv_ctx* c, const char* what, const void* data, int64_t seq_stride, int64_t head_stride, int64_t row_stride, int32_t n_kv_heads,
+                 int32_t head_dim) {
+  if (head_dim != 64 && head_dim != 128) return fail(c, CKV_ERR_SHAPE, "%s: head_dim %d unsupported (64 or 128)", what, head_dim);
+  if (n_kv_heads < 1 || n_kv_heads > 65535) return fail(c, CKV_ERR_SHAPE, "%s: n_kv_heads %d out of range", what, n_kv_heads);
+  if (!aligned16(data) || row_stride % 16 || head_stride % 16 || seq_stride % 16)
+    return fail(c, CKV_ERR_ARG, "%s: packed rows must be 16-byte aligned (strides multiples of 16)", what);
+  if (row_stride < CKV_PACKED_ROW_BYTES(head_dim) || head_stride < 0 || seq_stride < 0)
+    return fail(c, CKV_ERR_SHAPE, "%s: strides too small", what);
+  if (row_stride > INT_MAX) return fail(c, CKV_ERR_UNSUPPORTED, "%s: row_stride must stay below 2^31 bytes", what);
+  return CKV_OK;
+}
+
+int check_packed_view(ckv_ctx* c, const ckv_packed_view* kv) {
+  if (!kv || (kv->n_seq && (!kv->n_tokens || (kv->max_tokens && !kv->data))))
+    return fail(c, CKV_ERR_ARG, "caches: the view or one of its pointers is NULL");
+  if (int rc = check_packed(c, "caches", kv->data, kv->slot ? 0 : kv->seq_stride, kv->head_stride, kv->row_stride, kv->n_kv_heads, kv->head_dim))
+    return rc;
+  if (kv->n_seq < 0 || kv->n_seq > (1 << 20)) return fail(c, CKV_ERR_SHAPE, "caches: n_seq %d out of range", kv->n_seq);
+  if (kv->max_tokens < 0 || kv->max_tokens > INT_MAX - 1024)
+    return fail(c, CKV_ERR_SHAPE, "caches: max_tokens %d out of range", kv->max_tokens);
+  if (kv->slot && kv->pool_rows < 1) return fail(c, CKV_ERR_SHAPE, "caches: a paged view needs pool_rows >= 1");
+  if (kv->n_seq > 1 && ((kv->slot && kv->slot_stride < kv->max_tokens) || (kv->pos && kv->pos_stride < kv->max_tokens)))
+    return fail(c, CKV_ERR_SHAPE, "caches: slot and pos rows must hold max_tokens entries");
+  return CKV_OK;
+}
+
+// Keys and values in 16 bits, of n_seq sequences and n tokens each.
+int check_kv_rows(ckv_ctx* c, const ckv_kv_rows* r, int64_t seq_stride, const char* what) {
+  if (!r || !r->k || !r->v) return fail(c, CKV_ERR_ARG, "%s: NULL pointer", what);
+  if (r->dtype != CKV_BF16 && r->dtype != CKV_F16) return fail(c, CKV_ERR_ARG, "%s: unknown dtype %d", what, r->dtype);
+  if (!aligned16(r->k) || !aligned16(r->v) || r->tok_stride % 8 || r->head_stride % 8 || seq_stride % 8)
+    return fail(c, CKV_ERR_ARG, "%s: K/V rows must be 16-byte aligned (strides multiples of 8)", what);
+  if (r->tok_stride < 0 || r->head_stride < 0 || seq_stride < 0) return fail(c, CKV_ERR_SHAPE, "%s: strides must not be negative", what);
+  return CKV_OK;
+}
+
+// Whether no two rows of w elements share one: each axis (of more than one) steps over
+// all that the axes of shorter steps reach.
+struct Axis { int64_t n, st; };
+template <size_t N>
+bool rows_apart(int64_t w, Axis (&&ax)[N]) {
+  std::sort(ax, ax + N, [](const Axis& x, const Axis& y) { return x.st < y.st; });
+  for (const Axis& x : ax)
+    if (x.n > 1) {
+      if (x.st < w) return false;
+      w += extent(x.n, x.st);
+    }
+  return true;
+}
+
+SeqCaches make_caches(const ckv_packed_view* v) {
+  SeqCaches c;
+  c.k = reinterpret_cast<const uint16_t*>(v->data);
+  c.v = nullptr;
+  c.seq_stride = v->seq_stride / 2;
+  c.head_stride = v->head_stride / 2;
+  c.tok_stride = v->row_stride / 2;
+  c.slot = v->slot;
+  c.slot_stride = v->slot_stride;
+  c.pos = v->pos;
+  c.pos_stride = v->pos_stride;
+  c.n_tokens = v->n_tokens;
+  c.n_seq = v->n_seq;
+  c.max_tokens = v->max_tokens;
+  c.pool_last = v->slot ? v->pool_rows - 1 : 0;
+  return c;
+}
+
+}  // namespace
+
+extern "C" int ckv_pack_tokens(ckv_ctx* c, const ckv_kv_rows* in, const int32_t* row, int32_t n_rows, const int32_t* n_live,
+                               const ckv_packed_pool* pool) {
+  CKV_RANGE("ckv_pack_tokens");
+  if (!c) return CKV_ERR_ARG;
+  begin_call(c);
+  if (int rc0 = latched_nonfinite(c)) return rc0;
+  if (!pool) return fail(c, CKV_ERR_ARG, "pool: NULL pointer");
+  int rc;
+  if ((rc = check_packed(c, "pool", pool->data, 0, pool->head_stride, pool->row_stride, pool->n_kv_heads, pool->head_dim))) return rc;
+  if (n_rows < 0 || n_rows > INT_MAX - 1024) return fail(c, CKV_ERR_SHAPE, "n_rows %d out of range", n_rows);
+  if (pool->pool_rows < 0) return fail(c, CKV_ERR_SHAPE, "pool_rows %d out of range", pool->pool_rows);
+  if (n_rows == 0) return CKV_OK;
+  if ((rc = check_kv_rows(c, in, 0, "tokens"))) return rc;
+  if (!row) return fail(c, CKV_ERR_ARG, "row is NULL");
+  if (pool->pool_rows == 0) return CKV_OK;
+  if (!pool->data) return fail(c, CKV_ERR_ARG, "pool: NULL pointer");
+  const int64_t H = pool->n_kv_heads, d = pool->head_dim, bytes = CKV_PACKED_ROW_BYTES(d);
+  if (!rows_apart(bytes, {{pool->pool_rows, pool->row_stride}, {H, pool->head_stride}}))
+    return fail(c, CKV_ERR_SHAPE, "pool: rows of two heads overlap");
+  const size_t np = (size_t)(extent(pool->pool_rows, pool->row_stride) + extent(H, pool->head_stride) + bytes);
+  const size_t ni = (size_t)(extent(n_rows, in->tok_stride) + extent(H, in->head_stride) + d) * 2;
+  if (overlap(pool->data, np, in->k, ni) || overlap(pool->data, np, in->v, ni) || overlap(pool->data, np, row, (size_t)n_rows * 4) ||
+      overlap(pool->data, np, n_live, 4))
+    return fail(c, CKV_ERR_ARG, "the pool overlaps the tokens");
+  DeviceGuard g(c->device);
+  if (!g.ok) return fail(c, CKV_ERR_HIP, "cannot select device %d", c->device);
+  PackArgs a{};
+  a.k = in->k;
+  a.v = in->v;
+  a.head_stride = in->head_stride;
+  a.tok_stride = in->tok_stride;
+  a.f16 = in->dtype == CKV_F16;
+  a.pool = reinterpret_cast<char*>(pool->data);
+  a.pool_head = pool->head_stride;
+  a.pool_row = pool->row_stride;
+  a.Hkv = pool->n_kv_heads;
+  a.D = pool->head_dim;
+  a.row = row;
+  a.n_live = n_live;
+  a.n_rows = n_rows;
+  a.pool_rows = pool->pool_rows;
+  CKV_LAUNCH(c, "pack", launch_pack(a, c->stream));
+  return CKV_OK;
+}
+
+extern "C" int ckv_unpack_tokens(ckv_ctx* c, const ckv_packed_view* kv, const ckv_kv_rows* out) {
+  CKV_RANGE("ckv_unpack_tokens");
+  if (!c) return CKV_ERR_ARG;
+  begin_call(c);
+  if (int rc0 = latched_nonfinite(c)) return rc0;
+  int rc;
+  if ((rc = check_packed_view(c, kv))) return rc;
+  if (kv->n_seq == 0 || kv->max_tokens == 0) return CKV_OK;
+  if ((rc = check_kv_rows(c, out, out ? out->seq_stride : 0, "outputs"))) return rc;
+  const int64_t n = kv->n_seq, T = kv->max_tokens, H = kv->n_kv_heads, d = kv->head_dim;
+  if (!rows_apart(d, {{n, out->seq_stride}, {H, out->head_stride}, {T, out->tok_stride}}))
+    return fail(c, CKV_ERR_SHAPE, "outputs: rows overlap");
+  // (keys and values may alternate in one buffer)
+  const int64_t apart = std::abs(reinterpret_cast<intptr_t>(out->v) - reinterpret_cast<intptr_t>(out->k)) / 2;
+  if (!rows_apart(d, {{n, out->seq_stride}, {H, out->head_stride}, {T, out->tok_stride}, {2, apart}}))
+    return fail(c, CKV_ERR_ARG, "outputs overlap each other");
+  const size_t no = (size_t)(extent(n, out->seq_stride) + extent(H, out->head_stride) + extent(T, out->tok_stride) + d) * 2;
+  const size_t np = (size_t)((kv->slot ? 0 : extent(n, kv->seq_stride)) + extent(H, kv->head_stride) +
+                             extent(kv->slot ? kv->pool_rows : T, kv->row_stride) + CKV_PACKED_ROW_BYTES(d));
+  const size_t ns = (size_t)(extent(n, kv->slot_stride) + T) * 4;
+  for (const void* p : {(const void*)out->k, (const void*)out->v})
+    if (overlap(p, no, kv->data, np) || overlap(p, no, kv->slot, ns) || overlap(p, no, kv->n_tokens, n * 4))
+      return fail(c, CKV_ERR_ARG, "outputs overlap the caches");
+  DeviceGuard g(c->device);
+  if (!g.ok) return fail(c, CKV_ERR_HIP, "cannot select device %d", c->device);
+  PackArgs a{};
+  a.k = out->k;
+  a.v = out->v;
+  a.seq_stride = out->seq_stride;
+  a.head_stride = out->head_stride;
+  a.tok_stride = out->tok_stride;
+  a.f16 = out->dtype == CKV_F16;
+  a.pool = reinterpret_cast<char*>(const_cast<uint8_t*>(kv->data));
+  a.pool_seq = kv->seq_stride;
+  a.pool_head = kv->head_stride;
+  a.pool_row = kv->row_stride;
+  a.Hkv = kv->n_kv_heads;
+  a.D = kv->head_dim;
+  a.slot = kv->slot;
+  a.slot_stride = kv->slot_stride;
+  a.n_tokens = kv->n_tokens;
+  a.n_seq = kv->n_seq;
+  a.max_tokens = kv->max_tokens;
+  a.pool_last = kv->slot ? kv->pool_rows - 1 : 0;
+  CKV_LAUNCH(c, "unpack", launch_unpack(a, c->stream));
+  return CKV_OK;
+}
+
+extern "C" int ckv_attend_packed(ckv_ctx* c, const ckv_packed_view* kv, const ckv_query_view* q, int32_t dtype, int32_t window,
+                                 int32_t n_sink, void* o, float* lse) {
+  CKV_RANGE("ckv_attend_packed");
+  if (!c) return CKV_ERR_ARG;
+  begin_call(c);
+  if (int rc0 = latched_nonfinite(c)) return rc0;
+  int rc;
+  if ((rc = check_packed_view(c, kv))) return rc;
+  if (dtype != CKV_BF16 && dtype != CKV_F16) return fail(c, CKV_ERR_ARG, "unknown dtype %d", dtype);
+  if ((rc = check_query(c, q, kv->n_kv_heads, kv->head_dim, o, lse))) return rc;
+  if (window < 0 || n_sink < 0) return fail(c, CKV_ERR_ARG, "window %d and n_sink %d must not be negative", window, n_sink);
+  AttendArgs a;
+  a.own = make_caches(kv);
+  a.pre = a.own;
+  a.has_pre = false;
+  a.packed = true;
+  set_rows(c, a, q, kv->n_kv_heads, kv->head_dim, dtype, window, n_sink, o, lse);
+  return attend_rows(c, a, 0, kv->max_tokens);
 }

@@ -418,6 +418,102 @@ __device__ __forceinline__ void add_prefix(const AttendArgs& a, const PrefixPart
   });
 }
 
+// ---------------------------------------------------------------- few rows
+
+constexpr int kNarrowRows = 16;                     // rows of a block
+template <bool F16>
+constexpr int kNarrowLog = F16 ? 15 : 0;            // weights are formed this many powers of two as large
+
+template <bool F16>
+__device__ __forceinline__ f32x4 mfma16(u32x4 x, u32x4 y, f32x4 c) {
+  if constexpr (F16)
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, x), __builtin_bit_cast(f16x8, y), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), c, 0, 0, 0);
+}
+
+// over the four 16-lane rows of a wave: lanes l, l ^ 16, l ^ 32, l ^ 48
+__device__ __forceinline__ float max_rows16(float v) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return max32(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ __forceinline__ float sum_rows16(float v) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return sum32(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+
+// What the waves of a block of few rows left in LDS (wave w's weighted values
+// [16][D + 4] at tiles + w * wave_bytes, largest logits sm, sums sl), joined over
+// the waves, and over the block's splits by the one that finishes last.
+template <int D, bool F16, int NW>
+__device__ __forceinline__ void finish_block(const AttendArgs& a, const SplitSpace& sp, const PrefixParts& pp, const Item& it, int r0,
+                                             int n_rows, int g, const char* tiles, int wave_bytes, const float (&sm)[NW][kNarrowRows],
+                                             const float (&sl)[NW][kNarrowRows], int& last) {
+  constexpr int NT = 64 * NW, OP = D + 4;
+  const int tid = threadIdx.x;
+  __syncthreads();
+  auto finish = [&](int row, int w4, Joined j) {
+    const int rr = it.rb * kNarrowRows + row;
+    if (pp.n_split) {
+      const int first = row_start(a, 0), row = r0 + rr / a.group;     // (rows out of order may lie outside the prefix's)
+      if (row >= first && row < row_start(a, a.own.n_seq)) add_prefix(a, pp, D, (r0 - first) * a.group + rr, g, w4, j);
+    }
+    store_row<D, F16>(a, r0, rr, g, w4, j.acc, j.m, j.l);
+  };
+  constexpr int TPR = D / 4;                 // threads of a row, four widths each
+  const int64_t item = blockIdx.x;
+  for (int i = tid; i < n_rows * TPR; i += NT) {
+    const int row = i / TPR, w4 = (i % TPR) * 4;
+    float mm = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) mm = fmaxf(mm, sm[w][row]);
+    const float ref = mm == -INFINITY ? 0.f : mm;
+    float ll = 0.f;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float f = __builtin_amdgcn_exp2f(sm[w][row] - ref);
+      ll += f * sl[w][row];
+      acc += *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(tiles + w * wave_bytes) + row * OP + w4) * f;
+    }
+    if (it.n_split == 1) {
+      finish(row, w4, Joined{mm, ll, acc});
+    } else {
+      float* po = sp.o + (item * kNarrowRows + row) * D + w4;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) put_word(po + e, acc[e]);
+      if (w4 == 0) {
+        put_word(sp.ml + (item * kNarrowRows + row) * 2, mm);
+        put_word(sp.ml + (item * kNarrowRows + row) * 2 + 1, ll);
+      }
+    }
+  }
+  if (it.n_split == 1) return;
+  // the split that finishes last joins them all, in their order
+  const int64_t first = item - (int64_t)it.split * a.Hkv;
+  wait_own_stores();
+  __syncthreads();
+  if (tid == 0) {
+    const int before = __hip_atomic_fetch_add(sp.arrive + first, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    last = before == it.n_split - 1;
+    if (last) __hip_atomic_store(sp.arrive + first, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  __syncthreads();
+  if (!last) return;
+  for (int i = tid; i < n_rows * TPR; i += NT) {
+    const int row = i / TPR, w4 = (i % TPR) * 4;
+    Joined all = {-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f}};
+    all.template add_all<16>(it.n_split, [&](int k, float& m, float& l, f32x4& o) {
+      const int64_t at = (first + (int64_t)k * a.Hkv) * kNarrowRows + row;
+      m = get_word(sp.ml + at * 2);
+      l = get_word(sp.ml + at * 2 + 1);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = get_word(sp.o + at * D + w4 + e);
+    });
+    finish(row, w4, all);
+  }
+}
+
 }  // namespace
 
 }  // namespace ckv

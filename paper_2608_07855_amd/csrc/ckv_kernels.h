@@ -390,7 +390,8 @@ struct SeqCaches {
 struct AttendArgs {
   SeqCaches own, pre;     // pre: the shared tokens (one sequence), when has_pre
   bool has_pre;
-  bool f16;               // element type
+  bool f16;               // element type (packed: of queries and outputs)
+  bool packed;            // caches in 4 bits: `own.k` is the rows' first word, strides in 16-bit words, `own.v` unused
   const uint16_t* q;
   int64_t q_row_stride, q_head_stride;
   const int32_t* cu_rows;
@@ -456,5 +457,31 @@ struct SlotArgs {
   int32_t *n_tokens_out, *n_free_out, *cu_new, *new_row, *new_pos, *status;
 };
 hipError_t launch_slots(const SlotArgs& a, hipStream_t s);
+
+// ------------------------------------------------------- caches in 4 bits
+
+// keys and values in 16 bits and a pool (or caches) of packed rows
+struct PackArgs {
+  uint16_t* k;
+  uint16_t* v;
+  int64_t seq_stride, head_stride, tok_stride;   // elements
+  bool f16;
+  char* pool;
+  int64_t pool_seq, pool_head, pool_row;         // bytes
+  int Hkv, D;
+  // packing: token t goes to row[t]
+  const int32_t* row;
+  const int32_t* n_live;  // or null
+  int n_rows, pool_rows;
+  // reading back: token t of sequence s is row slot[s * slot_stride + t], or t
+  const int32_t* slot;
+  int64_t slot_stride;
+  const int32_t* n_tokens;
+  int n_seq, max_tokens, pool_last;
+};
+hipError_t launch_pack(const PackArgs& a, hipStream_t s);
+hipError_t launch_unpack(const PackArgs& a, hipStream_t s);
+// attention of few rows over packed caches (launch_attend_narrow calls it)
+hipError_t launch_packed_narrow(const AttendArgs& a, const AttendPlan& p, const SplitSpace& sp, hipStream_t s);
 
 }  // namespace ckv
