@@ -1860,7 +1860,7 @@ int attend_rows(ckv_ctx* c, const AttendArgs& a, int64_t n_pre, int64_t n_own) {
   if (a.n_rows == 0 || a.own.n_seq == 0) return CKV_OK;
   DeviceGuard g(c->device);
   if (!g.ok) return fail(c, CKV_ERR_HIP, "cannot select device %d", c->device);
-  bool few = a.packed || take_few(a, n_pre, n_own);
+  bool few = take_few(a, n_pre, n_own);
   AttendPlan p = few ? plan_narrow(a, n_own, true) : plan_wide(a, true);
   PrefixPlan pf = {0, 0, 0};
   if (a.has_pre && few) pf = plan_prefix(a);

@@ -38,27 +38,6 @@ struct PackedNarrow {
   static constexpr int kWaveB = kBuf * kTileB + 4 * 256;   // three buffers, four of slots and positions
 };
 
-// A row's 8 KS elements of the lane as fp16 times a power of two that brings the
-// row's largest to [2^14, 2^15); returns the inverse.  max_row: over the lanes of a row.
-template <int KS, class Max>
-__device__ __forceinline__ float queries_to_f16(u32x4 (&qf)[KS], Max max_row) {
-  float m = 0.f;
-#pragma unroll
-  for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(bf16_bits_to_float(chunk_elem(qf[ks], e))));
-  const uint32_t ex = max(__float_as_uint(max_row(m)) >> 23, 15u);
-  const float mul = __uint_as_float((268u - ex) << 23);
-#pragma unroll
-  for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const h2 v = {(_Float16)(bf16_bits_to_float(qf[ks][r] & 0xFFFFu) * mul), (_Float16)(__uint_as_float(qf[ks][r] & 0xFFFF0000u) * mul)};
-      qf[ks][r] = __builtin_bit_cast(uint32_t, v);
-    }
-  return __uint_as_float((ex - 14u) << 23);
-}
-
 template <int D, bool F16, bool TAB, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void attend_packed_narrow_kernel(AttendArgs a, SplitSpace sp, int target, int min_chunk, bool one_round) {
   using L = PackedNarrow<D, NW>;
@@ -324,10 +303,11 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_packed_narrow_kernel(Attend
         const char* row = rows_of + (slots ? (int)min((uint32_t)slots[t], (uint32_t)a.own.pool_last) : t) * row_bytes;
         float x = 0.f;
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks)
+        for (int ks = 0; ks < KS; ++ks) {
+          const u32x4 kk = row_values<D>(row, false, KS * q + ks);
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            x = fmaf(one_value<D>(row, false, D / 4 * q + 8 * ks + e), elem<true>(chunk_elem(qf[ks], e)), x);
+          for (int e = 0; e < 8; ++e) x = fmaf(elem<true>(chunk_elem(kk, e)), elem<true>(chunk_elem(qf[ks], e)), x);
+        }
         x = product(sum_rows16(x), row_sl2);
         if (!sees(poss ? poss[t] : t, qp, a.window, a.n_sink)) continue;
         const float nm = fmaxf(m, x), ref = nm == -INFINITY ? 0.f : nm;
@@ -335,9 +315,11 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_packed_narrow_kernel(Attend
         m = nm;
         l = l * al + (q == 0 ? w : 0.f);
 #pragma unroll
-        for (int j = 0; j < JW; ++j)
+        for (int r = 0; r < 4; ++r) {
+          const u32x4 y = row_values<D>(row, true, JW * (4 * q + r) / 8);
 #pragma unroll
-          for (int r = 0; r < 4; ++r) o[j][r] = fmaf(w, one_value<D>(row, true, JW * (4 * q + r) + j), o[j][r] * al);
+          for (int j = 0; j < JW; ++j) o[j][r] = fmaf(w, half_of(y[(JW * r % 8 + j) / 2], j % 2), o[j][r] * al);
+        }
       }
     }
   }

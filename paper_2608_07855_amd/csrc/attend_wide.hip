@@ -1,6 +1,7 @@
 // Attention of ragged batches, many rows at a time: prompts, chunks, and the
 // rows of a whole batch over the tokens that it shares.
 #include "attend_device.h"
+#include "packed_device.h"
 
 #include <algorithm>
 
@@ -64,6 +65,8 @@ struct Wide {
   static constexpr int kOwn = LOADS * LANES;           // tokens of a tile that a wave loads
   static constexpr int kRowB = 2 * D, kTileB = kTok * kRowB;
   static constexpr int kLds = 6 * kTileB + kNW * 4 * 256;   // three tiles of K, three of V, four tables a wave
+  // caches in 4 bits: a wave's rows of four tiles more, as they are in memory
+  static constexpr int kRawB = kOwn * PackedRow<D>::kBytes, kRawChunks = kRawB / 16, RAW_LOADS = (kRawChunks + 63) / 64;
 };
 
 template <bool F16>
@@ -260,11 +263,18 @@ enum Kept { kS, kRb, kR0, kRows, kX0, kX1 = kX0 + 2, kWork = kX1 + 2, kQmin = kW
 // PRE: the rows of all sequences over the shared tokens, in n_split splits, as
 // partial sums.  Otherwise a share of the blocks (W shares a KV head), in each
 // the shared tokens first; n_split 1: whole blocks only.
-template <int D, bool F16, bool TAB, bool PRE>
+//
+// PACK: caches in 4 bits.  Direct loads bring a wave's rows of a tile to LDS as they
+// are; two tiles before their products the wave makes fp16 of them and writes
+// them where a 16-bit tile would have been loaded, for all waves: a 256th of the
+// block's rows' work a token instead of one in each wave.  All products are fp16;
+// bf16 queries become fp16 times a power of two of their row's own.
+template <int D, bool F16, bool TAB, bool PRE, bool PACK>
 __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, SplitSpace sp, int W, int n_split) {
   using L = Wide<D>;
+  constexpr bool C16 = F16 || PACK;        // what the products take
   constexpr int KS = D / 16, DB = D / 32;
-  __shared__ __align__(256) char tiles[L::kLds];
+  __shared__ __align__(256) char tiles[L::kLds + (PACK ? kNW * 4 * L::kRawB : 0)];
   __shared__ ShareShared ssh;
   __shared__ int qlim[2][kNW];
   // What a block needs again behind its tiles waits in LDS (a copy a wave), and
@@ -364,6 +374,8 @@ __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, Sp
     const uint16_t* qr = a.q + (int64_t)(r0 + p) * a.q_row_stride + (int64_t)h * a.q_head_stride;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) qf[ks] = ldg_u4(qr + 16 * ks + 8 * hf);
+    float back = 1.f;             // the row's logits are its products times this
+    if constexpr (PACK && !F16) back = queries_to_f16<KS>(qf, [](float v) { return max32(v); });
     int qmin = qp, qmax = qp;
 #pragma unroll
     for (int off = 16; off; off >>= 1) {
@@ -472,7 +484,7 @@ __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, Sp
       const AttendArgs& a = fresh();
       const SeqCaches& kv = k ? a.own : a.pre;
       const Part pt = open(k);
-      const float sl2 = a.sl2;
+      const float sl2 = a.sl2 * back;
       const Range rg = pt.rg;
       const int tile0 = pt.tile0, tile1 = pt.tile1;
       const int64_t head = g * kv.head_stride + (kv.slot ? 0 : pt.sq * kv.seq_stride);
@@ -522,6 +534,59 @@ __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, Sp
         load_rows(rows, vh, vc, (2 * L::LANES & (L::CH - 1)) << 4, lds + (3 + tile % 3) * L::kTileB);
       };
 
+      // 4 bits: 16-byte chunk x = 64 j + lane of the wave's part of a tile is chunk x % CH of its row x / CH
+      using R = PackedRow<D>;
+      const uint32_t raw = tab - wave * 4 * 256 + kNW * 4 * 256 + wave * 4 * L::kRawB;
+      // (the lane is opaque, or what both derive from it is kept in registers through the tiles)
+      auto load_raw = [&](int tile) {
+        int ln = lane;
+        asm volatile("" : "+v"(ln));
+        uint32_t rows[L::RAW_LOADS];
+#pragma unroll
+        for (int j = 0; j < L::RAW_LOADS; ++j) {
+          const int r = min(64 * j + ln, L::kRawChunks - 1) / R::CH;
+          if (TAB && slots) {
+            const auto* w = (const __attribute__((address_space(3))) int*)(uintptr_t)(tab + (tile & 3) * 256);
+            rows[j] = min((uint32_t)w[r], (uint32_t)kv.pool_last);
+          } else {
+            rows[j] = token(tile, wave * L::kOwn + r);
+          }
+        }
+        wait_lds_reads();
+        const uint32_t to = raw + (tile & 3) * L::kRawB;
+#pragma unroll
+        for (int j = 0; j < L::RAW_LOADS; ++j) {
+          const int x = 64 * j + ln;
+          if (L::kRawChunks % 64 && x >= L::kRawChunks) continue;
+          const uint32_t in = x % R::CH * 16;
+          if (near) load_lds16_near(kh, __umul24(rows[j], row_bytes) + in, to + j * 1024);
+          else load_lds16(kh + ((uint64_t)rows[j] * row_bytes + in), to + j * 1024);
+        }
+      };
+      // eight lanes a row: lane i % 8 has widths D/4 (i % 4) .. of its key (i % 8 < 4) or value
+      auto make_tile = [&](int tile) {
+        int ln = lane;
+        asm volatile("" : "+v"(ln));
+        const int row = ln >> 3, part = ln & 3, value = (ln >> 2) & 1, r = wave * L::kOwn + row;
+        const uint32_t from = raw + (tile & 3) * L::kRawB + row * R::kBytes;
+        const auto word = [](uint32_t at) { return *(const __attribute__((address_space(3))) uint32_t*)(uintptr_t)at; };
+        const Scale sc = scale_of(word(from + R::kParams + value * (D / 8) + D / 4 * part / 32 * 4));
+        uint32_t w[D / 32];
+        const uint32_t at = from + value * R::kValue + D / 8 * part;
+        if constexpr (D == 128) {
+          const u32x4 c4 = lds_read16(at);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) w[i] = c4[i];
+        } else {
+          w[0] = word(at);
+          w[1] = word(at + 4);
+        }
+        const uint32_t to = lds + (value * 3 + tile % 3) * L::kTileB + r * L::kRowB, mix = (r << value) & (L::CH - 1);
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i)
+          *(__attribute__((address_space(3))) u32x4*)(uintptr_t)(to + (((D / 32 * part + i) ^ mix) << 4)) = eight_values(w[i], sc);
+      };
+
       // scores of a tile (raw products)
       auto score = [&](int tile, f32x16 (&x)[2]) {
         const uint32_t off = (tile % 3) * L::kTileB;
@@ -531,7 +596,7 @@ __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, Sp
 #pragma unroll
           for (int ks = 0; ks < KS; ++ks) {
             const u32x4 kf = lds_read16((ka + off) ^ (32 * ks), tb * 32 * L::kRowB);
-            x[tb] = mfma32<F16>(kf, qf[ks], x[tb]);
+            x[tb] = mfma32<C16>(kf, qf[ks], x[tb]);
           }
         }
       };
@@ -565,7 +630,7 @@ __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, Sp
       // early; the fences keep the compiler from gathering either.
       auto step = [&](int t, f32x16 (&x)[2], float& mx, f32x16 (&y)[2], float& my) {
         const float top = max32(mx) * sl2;
-        if (__ballot(top > m + kLag<F16> || (m == -INFINITY && top > m)) != 0ull) {
+        if (__ballot(top > m + kLag<C16> || (m == -INFINITY && top > m)) != 0ull) {
           const float nm = top > m ? top : m;
           const float al = nm == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - nm);
           l *= al;
@@ -583,7 +648,7 @@ __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, Sp
           ref = 0.f;
           mul = 1.f;
         }
-        ref -= kWeightLog<F16>;
+        ref -= kWeightLog<C16>;
         u32x4 ph[4];
         float lt = 0.f;       // the tile's sum: small weights add up before they meet a large l
         {
@@ -596,7 +661,7 @@ __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, Sp
           __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
           for (int j = 0; j < 2 * KS; ++j) {
-            y[j % 2] = mfma32<F16>(kf[j % kAhead], qf[j / 2], j < 2 ? zero16() : y[j % 2]);
+            y[j % 2] = mfma32<C16>(kf[j % kAhead], qf[j / 2], j < 2 ? zero16() : y[j % 2]);
             if (j + kAhead < 2 * KS) kf[j % kAhead] = read(j + kAhead);
             // the tile's 16 pairs of scores, over the 2 KS products
 #pragma unroll
@@ -605,7 +670,7 @@ __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, Sp
               const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[tb][r], mul, -ref));
               const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[tb][r + 1], mul, -ref));
               lt = q ? lt + (p0 + p1) : p0 + p1;
-              ph[q / 4][q % 4] = pack2<F16>(p0, p1);
+              ph[q / 4][q % 4] = pack2<C16>(p0, p1);
             }
             __builtin_amdgcn_sched_barrier(0);
           }
@@ -630,7 +695,7 @@ __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, Sp
           __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
           for (int j = 0; j < 4 * DB; ++j) {
-            o[j % DB] = mfma32<F16>(vf[j % kAhead], ph[j / DB], o[j % DB]);
+            o[j % DB] = mfma32<C16>(vf[j % kAhead], ph[j / DB], o[j % DB]);
             if (j + kAhead < 4 * DB) vf[j % kAhead] = read(j + kAhead);
 #pragma unroll
             for (int q = j * 16 / (4 * DB); q < (j + 1) * 16 / (4 * DB); ++q)
@@ -646,10 +711,17 @@ __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, Sp
       if (tile0 < tile1) {
         if (k == 1 && has_pre) tile_barrier();     // the shared tokens' tiles have been read
 #pragma unroll
-        for (int j = 0; j < 3; ++j)
+        for (int j = 0; j < (PACK ? 4 : 3); ++j)
           if (tile0 + j < tile1) load_tables(tile0 + j);
         if (TAB) wait_loads<0>();
         uint32_t rows[L::LOADS], ahead[L::LOADS];
+        if constexpr (PACK) {
+#pragma unroll
+          for (int j = 0; j < 3; ++j)
+            if (tile0 + j < tile1) load_raw(tile0 + j);
+          if (tile0 + 4 < tile1) load_tables(tile0 + 4);
+          if (tile0 + 3 < tile1) load_raw(tile0 + 3);
+        } else {
         find_rows(tile0, rows);
         load_k(tile0, rows);
         if (tile0 + 1 < tile1) {
@@ -665,15 +737,46 @@ __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, Sp
           }
           load_v(tile0 + 1, ahead);
         }
+        }
         // What the compiler loaded has to have arrived before the loop, or its own
         // waits inside would drain the tiles under way.
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qf[ks]));
         asm volatile("" : "+v"(qp));
+        if constexpr (PACK) {
+          wait_loads<0>();
+          make_tile(tile0);
+          if (tile0 + 1 < tile1) make_tile(tile0 + 1);
+        }
         f32x16 xa[2], xb[2];
         float ma, mb;
         // under way, oldest first: step t, tables(t + 3), step t + 1; rows: of tile t + 2
+        // (4 bits: rows of tile t + 2, tables(t + 4), rows of t + 3; tiles t and t + 1 are made)
         auto turn = [&](int t, bool first, f32x16 (&x)[2], float& mx, f32x16 (&y)[2], float& my) {
+          if constexpr (PACK) {
+            tile_barrier();           // tile t + 1 is there, and no wave reads tile t - 1 any more
+            if (first && wave_on) {
+              score(t, x);
+              mask(t, x);
+              mx = -INFINITY;
+#pragma unroll
+              for (int r = 0; r < 16; ++r) mx = max3(mx, x[0][r], x[1][r]);
+            }
+            if (t + 2 < tile1) {
+              if (t + 5 < tile1) {
+                load_tables(t + 5);
+                wait_loads<L::RAW_LOADS + T>();
+              } else if (t + 3 < tile1) {
+                wait_loads<L::RAW_LOADS>();
+              } else {
+                wait_loads<0>();
+              }
+              if (t + 4 < tile1) load_raw(t + 4);
+              make_tile(t + 2);
+            }
+            if (wave_on) step(t, x, mx, y, my);
+            return;
+          }
           if (t + 3 < tile1) wait_loads<T + KV>();
           else if (t + 2 < tile1) wait_loads<KV>();
           else if (t + 1 < tile1) wait_loads<L::LOADS>();
@@ -733,8 +836,8 @@ __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, Sp
       record = make_int4(get(kRecord), get(kRecord + 1), get(kRecord + 2), get(kRecord + 3));
     }
     l = sum32(l);
-    if constexpr (kWeightLog<F16> > 0) {
-      constexpr float back = 1.f / (1 << kWeightLog<F16>);
+    if constexpr (kWeightLog<C16> > 0) {
+      constexpr float back = 1.f / (1 << kWeightLog<C16>);
       l *= back;
 #pragma unroll
       for (int db = 0; db < DB; ++db) o[db] *= back;
@@ -763,11 +866,13 @@ __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, Sp
           float x = 0.f;
 #pragma unroll
           for (int ks = 0; ks < KS; ++ks) {
-            const u32x4 kk = ldg_u4(kv.k + at + 16 * ks + 8 * hf2);
+            u32x4 kk;
+            if constexpr (PACK) kk = row_values<D>(reinterpret_cast<const char*>(kv.k + at), false, 2 * ks + hf2);
+            else kk = ldg_u4(kv.k + at + 16 * ks + 8 * hf2);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x = fmaf(elem<F16>(chunk_elem(kk, j)), elem<F16>(chunk_elem(qf[ks], j)), x);
+            for (int j = 0; j < 8; ++j) x = fmaf(elem<C16>(chunk_elem(kk, j)), elem<C16>(chunk_elem(qf[ks], j)), x);
           }
-          x = product(sum32(x), b.sl2);
+          x = product(sum32(x), b.sl2 * back);
           if (!(t < pt.row_hi && (t >= pt.row_lo || t < pt.rg.n_first))) continue;
           const float nm = fmaxf(m, x), ref = nm == -INFINITY ? 0.f : nm;
           const float al = __builtin_amdgcn_exp2f(m - ref), p = __builtin_amdgcn_exp2f(x - ref);
@@ -776,8 +881,16 @@ __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, Sp
 #pragma unroll
           for (int db = 0; db < DB; ++db)
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-              o[db][r] = fmaf(p, elem<F16>(kv.v[at + 32 * db + 8 * (r / 4) + 4 * hf2 + r % 4]), o[db][r] * al);
+            for (int r = 0; r < 16; ++r) {
+              float v;
+              if constexpr (PACK) {
+                const u32x4 y = row_values<D>(reinterpret_cast<const char*>(kv.k + at), true, 4 * db + r / 4);
+                v = half_of(hf2 ? y[2 + r % 4 / 2] : y[r % 4 / 2], r % 2);
+              } else {
+                v = elem<F16>(kv.v[at + 32 * db + 8 * (r / 4) + 4 * hf2 + r % 4]);
+              }
+              o[db][r] = fmaf(p, v, o[db][r] * al);
+            }
         }
       }
     }
@@ -908,7 +1021,7 @@ PrefixPlan plan_prefix(const AttendArgs& a) {
   return p;
 }
 
-#define CKV_WIDE(D, F16, TAB, PRE, GRID, W, K) attend_wide_kernel<D, F16, TAB, PRE><<<GRID, kNT, 0, s>>>(a, sp, W, K)
+#define CKV_WIDE(D, F16, TAB, PRE, GRID, W, K) attend_wide_kernel<D, F16, TAB, PRE, kPack><<<GRID, kNT, 0, s>>>(a, sp, W, K)
 #define CKV_WIDE3(D, F16, PRE, GRID, W, K) \
   if (tab) CKV_WIDE(D, F16, true, PRE, GRID, W, K); \
   else CKV_WIDE(D, F16, false, PRE, GRID, W, K)
@@ -922,13 +1035,20 @@ PrefixPlan plan_prefix(const AttendArgs& a) {
 hipError_t launch_attend_wide(const AttendArgs& a, const AttendPlan& p, const SplitSpace& sp, hipStream_t s) {
   const dim3 grid((unsigned)p.grid);
   const bool tab = a.own.slot || (a.has_pre && a.pre.slot);
-  CKV_WIDE2(false, grid, p.target, p.split ? 0 : 1)
+  if (a.packed) {
+    constexpr bool kPack = true;
+    CKV_WIDE2(false, grid, p.target, p.split ? 0 : 1)
+  } else {
+    constexpr bool kPack = false;
+    CKV_WIDE2(false, grid, p.target, p.split ? 0 : 1)
+  }
   return hipGetLastError();
 }
 
 hipError_t launch_attend_prefix(const AttendArgs& a, const PrefixPlan& p, const SplitSpace& sp, hipStream_t s) {
   const dim3 grid((unsigned)(p.blocks * p.n_split * a.Hkv));
   const bool tab = a.pre.slot != nullptr;
+  constexpr bool kPack = false;
   CKV_WIDE2(true, grid, 0, p.n_split)
   return hipGetLastError();
 }

@@ -55,15 +55,34 @@ __device__ __forceinline__ u32x4 eight_values(uint32_t w, const Scale& c) {
   return u32x4{two_values<0>(w, c), two_values<1>(w, c), two_values<2>(w, c), two_values<3>(w, c)};
 }
 
-// One width of a key (or value) of a row in memory.
+// Widths 8j to 8j+7 of a key (or value) of a row in memory.
 template <int D>
-__device__ __forceinline__ float one_value(const char* row, bool value, int w) {
-  const int j = w / 8, p = w % 8 / 2, h = w % 2;
+__device__ __forceinline__ u32x4 row_values(const char* row, bool value, int j) {
   const uint32_t word = ldg_i32(row + (value ? PackedRow<D>::kValue : 0) + 4 * j);
-  const uint32_t par = ldg_i32(row + (value ? PackedRow<D>::kValueParams : PackedRow<D>::kParams) + w / 32 * 4);
-  const h2 n = __builtin_bit_cast(h2, ((word >> (4 * p + 16 * h) & 15u) << 6) | 0x4C00u);
-  const Scale c = scale_of(par);
-  return (float)__builtin_elementwise_fma(n, c.s, c.b)[0];
+  return eight_values(word, scale_of(ldg_i32(row + (value ? PackedRow<D>::kValueParams : PackedRow<D>::kParams) + j / 4 * 4)));
+}
+// the fp16 number in one half of a word
+__device__ __forceinline__ float half_of(uint32_t w, int h) { return (float)__builtin_bit_cast(h2, w)[h]; }
+
+// A row's 8 KS elements of the lane as fp16 times a power of two that brings the
+// row's largest to [2^14, 2^15); returns the inverse.  max_row: over the lanes of a row.
+template <int KS, class Max>
+__device__ __forceinline__ float queries_to_f16(u32x4 (&qf)[KS], Max max_row) {
+  float m = 0.f;
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(bf16_bits_to_float(chunk_elem(qf[ks], e))));
+  const uint32_t ex = max(__float_as_uint(max_row(m)) >> 23, 15u);
+  const float mul = __uint_as_float((268u - ex) << 23);
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const h2 v = {(_Float16)(bf16_bits_to_float(qf[ks][r] & 0xFFFFu) * mul), (_Float16)(__uint_as_float(qf[ks][r] & 0xFFFF0000u) * mul)};
+      qf[ks][r] = __builtin_bit_cast(uint32_t, v);
+    }
+  return __uint_as_float((ex - 14u) << 23);
 }
 
 }  // namespace
