@@ -1826,6 +1826,15 @@ bool take_few(const AttendArgs& a, int64_t n_pre, int64_t n_own) {
   const int64_t n = std::min(a.own.n_seq, a.n_rows), rows = (int64_t)a.max_rows * a.group;
   const double blocks = (double)((rows + 15) / 16), wide = (double)((rows + 255) / 256);
   if (a.window) n_own = std::min(n_own, (int64_t)a.window + a.n_sink + a.max_rows);
+  if (a.packed) {
+    // In 4 bits a token costs the few-rows kernel more of a compute unit's time for each 16
+    // rows, the many-rows kernel hardly more than its products.  Microseconds, fitted to
+    // 16 sequences of 8192 tokens, 8 KV heads (32 rows 90 and 127, 64 rows 171 and 131) and
+    // 4 of 512 (64 rows 16 and 26); a block of 256 rows that falls into many shares waits for
+    // their join (144 rows of one head on 65536 tokens 44 and 344).
+    const double tokens = (double)n * a.Hkv * n_own * 1e-6, shares = std::min(256.0, tokens * wide * 1e6 / 256);
+    return blocks * tokens * 41 <= wide * tokens * 118 + 12 + 1.3 * std::max(0.0, shares / (n * wide * a.Hkv) - 1);
+  }
   if (!a.has_pre) return blocks <= 1 || n * blocks * a.Hkv * n_own <= 512 * 256;
   const double packed = (double)(((int64_t)a.n_rows * a.group + 255) / 256);
   return packed * n_pre + n * std::max(1.0, 0.7 * blocks) * n_own <= n * wide * (double)(n_pre + n_own);

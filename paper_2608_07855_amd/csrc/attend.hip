@@ -354,7 +354,18 @@ AttendPlan plan_narrow(const AttendArgs& a, int64_t max_tokens, bool room) {
   const int64_t seen = a.window ? std::min(max_tokens, (int64_t)a.window + a.n_sink + a.max_rows) : max_tokens;
   p.min_chunk = small ? 256 : 2048;
   int64_t e = p.target / a.Hkv + blocks + 1;
-  if (!room || seen <= (small ? 512 : 2048) || blocks * a.Hkv >= 4 * p.target) {
+  if (a.packed) {
+    // Caches in 4 bits: 12 waves a compute unit either way, as one workgroup or as three.
+    // Many row blocks: twice as many splits as run at a time (64 long ragged sequences
+    // 290 us; with 1024 splits 310, with 3072 290).  Few: splits of 256 tokens for
+    // short caches, up to 16 of them (what is joined at once), 768 tokens for long
+    // ones (one cache of 8192 tokens 21.7 us, in 32 splits 27.7).  Caches up to 2048
+    // tokens stay whole where blocks are not few (16 of 1024 tokens 13.1 us, in halves 16.4; 4224: 30, whole 35).
+    if (!p.alone) p.target = 1536;
+    p.min_chunk = small ? (int)std::min<int64_t>(std::max<int64_t>(seen / 16, 256), 768) : p.alone ? 2048 : 1024;
+    e = p.target / a.Hkv + blocks + 1;
+  }
+  if (!room || seen <= (small ? 512 : 2048) || blocks * a.Hkv >= 4096) {
     p.min_chunk = INT_MAX;                                              // no splits
     e = blocks;
   }

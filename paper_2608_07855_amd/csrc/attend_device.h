@@ -68,6 +68,20 @@ __device__ __forceinline__ uint16_t to_elem(float x) {
   else return __builtin_bit_cast(uint16_t, (__bf16)x);
 }
 
+// two values rounded to the type, packed
+template <bool F16>
+__device__ __forceinline__ uint32_t pack2(float x, float y) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  const f32x2 v = {x, y};
+  if constexpr (F16) {
+    typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, h2));
+  } else {
+    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, b2));
+  }
+}
+
 // ---------------------------------------------------------------------------
 // Work items.  A sequence's query rows of one KV head (position by position,
 // the head's group of query heads innermost) are cut into blocks, and the
@@ -316,6 +330,14 @@ __device__ __forceinline__ void load_lds16_near(const void* g, uint32_t offset, 
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(lds)),
                "v"(offset), "s"(uniform((long long)(uintptr_t)g)) : "m0", "memory");
 }
+// the same two past the caches' lines for good (bytes that are read once)
+__device__ __forceinline__ void load_lds16_once(const void* g, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(g) : "m0", "memory");
+}
+__device__ __forceinline__ void load_lds16_near_once(const void* g, uint32_t offset, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(__builtin_amdgcn_readfirstlane(lds)),
+               "v"(offset), "s"(uniform((long long)(uintptr_t)g)) : "m0", "memory");
+}
 __device__ __forceinline__ void load_lds4(const void* g, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(g) : "m0", "memory");
 }
@@ -444,8 +466,11 @@ __device__ __forceinline__ float sum_rows16(float v) {
 
 // What the waves of a block of few rows left in LDS (wave w's weighted values
 // [16][D + 4] at tiles + w * wave_bytes, largest logits sm, sums sl), joined over
-// the waves, and over the block's splits by the one that finishes last.
-template <int D, bool F16, int NW>
+// the waves, and over the block's splits by the one that finishes last.  TREE: of
+// more than 16 splits each 16 are joined first, by whichever finishes last of
+// them, and these sums by the last of those (a split's sums are 8 KB and more, which one
+// workgroup reads at 0.4 us a split: 256 splits of one cache 131 us, in a tree %TREE%).
+template <int D, bool F16, int NW, bool TREE = false>
 __device__ __forceinline__ void finish_block(const AttendArgs& a, const SplitSpace& sp, const PrefixParts& pp, const Item& it, int r0,
                                              int n_rows, int g, const char* tiles, int wave_bytes, const float (&sm)[NW][kNarrowRows],
                                              const float (&sl)[NW][kNarrowRows], int& last) {
@@ -491,26 +516,61 @@ __device__ __forceinline__ void finish_block(const AttendArgs& a, const SplitSpa
   if (it.n_split == 1) return;
   // the split that finishes last joins them all, in their order
   const int64_t first = item - (int64_t)it.split * a.Hkv;
-  wait_own_stores();
-  __syncthreads();
-  if (tid == 0) {
-    const int before = __hip_atomic_fetch_add(sp.arrive + first, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    last = before == it.n_split - 1;
-    if (last) __hip_atomic_store(sp.arrive + first, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  }
-  __syncthreads();
-  if (!last) return;
-  for (int i = tid; i < n_rows * TPR; i += NT) {
-    const int row = i / TPR, w4 = (i % TPR) * 4;
+  // Whether this workgroup is the last of n to arrive at split k's count (which is zero again then)
+  auto last_of = [&](int n, int k) {
+    wait_own_stores();
+    __syncthreads();
+    if (tid == 0) {
+      int* count = sp.arrive + first + (int64_t)k * a.Hkv;
+      const int before = __hip_atomic_fetch_add(count, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      last = before == n - 1;
+      if (last) __hip_atomic_store(count, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    return last != 0;
+  };
+  // widths w4 .. of a row, over the sums of n splits, k0 and every step-th after it
+  auto joined = [&](int row, int w4, int k0, int step, int n) {
     Joined all = {-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f}};
-    all.template add_all<16>(it.n_split, [&](int k, float& m, float& l, f32x4& o) {
-      const int64_t at = (first + (int64_t)k * a.Hkv) * kNarrowRows + row;
+    all.template add_all<16>(n, [&](int k, float& m, float& l, f32x4& o) {
+      const int64_t at = (first + (int64_t)(k0 + k * step) * a.Hkv) * kNarrowRows + row;
       m = get_word(sp.ml + at * 2);
       l = get_word(sp.ml + at * 2 + 1);
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[e] = get_word(sp.o + at * D + w4 + e);
     });
-    finish(row, w4, all);
+    return all;
+  };
+  int n = it.n_split, step = 1;
+  if (TREE && n > 16) {
+    const int k0 = it.split & ~15, members = min(16, n - k0);
+    // (split k0 + 1's count is the group's; a group of one has no other to wait for)
+    if (members > 1 && !last_of(members, k0 + 1)) return;
+    if (members > 1) {
+      static_assert(NT % TPR == 0);                  // a row's threads take it in the same turn
+      for (int i0 = 0; i0 < n_rows * TPR; i0 += NT) {
+        const int i = i0 + tid, row = i / TPR, w4 = (i % TPR) * 4;
+        Joined all;
+        if (i < n_rows * TPR) all = joined(row, w4, k0, 1, members);
+        __syncthreads();                             // the row's largest logit and sum have been read
+        if (i < n_rows * TPR) {
+          const int64_t at = (first + (int64_t)k0 * a.Hkv) * kNarrowRows + row;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) put_word(sp.o + at * D + w4 + e, all.acc[e]);
+          if (w4 == 0) {
+            put_word(sp.ml + at * 2, all.m);
+            put_word(sp.ml + at * 2 + 1, all.l);
+          }
+        }
+      }
+    }
+    step = 16;
+    n = (n + 15) / 16;
+  }
+  if (!last_of(n, 0)) return;
+  for (int i = tid; i < n_rows * TPR; i += NT) {
+    const int row = i / TPR, w4 = (i % TPR) * 4;
+    finish(row, w4, joined(row, w4, 0, step, n));
   }
 }
 

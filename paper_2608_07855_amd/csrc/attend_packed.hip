@@ -32,14 +32,14 @@ template <int D, int NW_>
 struct PackedNarrow {
   using R = PackedRow<D>;
   static constexpr int NW = NW_, NT = 64 * NW;
-  static constexpr int kTok = 32, kBuf = 3;
+  static constexpr int kTok = 32, kBuf = 2;
   static constexpr int kTileB = kTok * R::kBytes, kChunks = kTileB / 16;
   static constexpr int LOADS = (kChunks + 63) / 64;     // loads of a tile
-  static constexpr int kWaveB = kBuf * kTileB + 4 * 256;   // three buffers, four of slots and positions
+  static constexpr int kWaveB = kBuf * kTileB + 4 * 256;   // two buffers, four of slots and positions
 };
 
 template <int D, bool F16, bool TAB, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void attend_packed_narrow_kernel(AttendArgs a, SplitSpace sp, int target, int min_chunk, bool one_round) {
+__global__ __launch_bounds__(64 * NW, 3) void attend_packed_narrow_kernel(AttendArgs a, SplitSpace sp, int target, int min_chunk, bool one_round) {
   using L = PackedNarrow<D, NW>;
   using R = PackedRow<D>;
   constexpr int NT = L::NT, KS = D / 32, JW = D / 16;
@@ -83,44 +83,58 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_packed_narrow_kernel(Attend
   rg.ns = __builtin_amdgcn_readfirstlane(rg.ns);
   rg.shift = __builtin_amdgcn_readfirstlane(rg.shift);
   rg.cnt = __builtin_amdgcn_readfirstlane(rg.cnt);
-  // the split's tokens, and the wave's among them (whole tiles)
+  // the split's tokens, and the wave's among them: every NW-th tile, so that what
+  // the workgroup reads at a time lies together
   const int n_tiles = (rg.cnt + L::kTok - 1) / L::kTok;
   const int per_split = (n_tiles + it.n_split - 1) / it.n_split;
   const int t_begin = min(it.split * per_split, n_tiles), t_end = min(t_begin + per_split, n_tiles);
-  const int per_wave = (t_end - t_begin + NW - 1) / NW;
-  const int tile0 = min(t_begin + wave * per_wave, t_end), tile1 = min(tile0 + per_wave, t_end);
+  const int tile0 = t_begin + wave, my_tiles = max(t_end - tile0 + NW - 1, 0) / NW;
 
   const uint32_t my = lds_at(tiles) + wave * L::kWaveB, tab = my + L::kBuf * L::kTileB;
-  const char* rows_of = reinterpret_cast<const char*>(a.own.k + g * a.own.head_stride + (a.own.slot ? 0 : s * a.own.seq_stride));
+  const char* rows_of = reinterpret_cast<const char*>(
+      uniform((long long)(uintptr_t)(a.own.k + g * a.own.head_stride + (a.own.slot ? 0 : s * a.own.seq_stride))));
   const int32_t* slots = a.own.slot ? a.own.slot + s * a.own.slot_stride : nullptr;
   const int32_t* poss = a.own.pos ? a.own.pos + s * a.own.pos_stride : nullptr;
   const int64_t row_bytes = a.own.tok_stride * 2;
-
+  // rows that 32-bit offsets reach (24-bit products) take one instruction each
+  const int last_row = slots ? a.own.pool_last : max(n - 1, 0);
+  const bool near = (uint64_t)last_row * row_bytes + row_bytes < (1ull << 32) && last_row < (1 << 24) && row_bytes < (1 << 24);
   auto token = [&](int tile, int r) { return rg.token(min(tile * L::kTok + r, rg.cnt - 1)); };
   auto word_at = [](uint32_t at) { return *(const __attribute__((address_space(3))) uint32_t*)(uintptr_t)at; };
   // slots (lanes 0-31) and positions (lanes 32-63) of a tile; without one of the tables its lanes read the other
-  auto load_tables = [&](int tile) {
+  auto load_tables = [&](int i) {
     if constexpr (TAB) {
+      const int tile = tile0 + i * NW;
       const int32_t* from = lane < 32 ? (slots ? slots : poss) : (poss ? poss : slots);
-      load_lds4(from + token(tile, lane & 31), tab + (tile & 3) * 256);
+      load_lds4(from + token(tile, lane & 31), tab + (i & 3) * 256);
     }
   };
-  // 16-byte chunk x = 64 i + lane of a tile is chunk x % CH of token x / CH
-  auto load_tile = [&](int tile) {
-    const uint32_t to = my + tile % L::kBuf * L::kTileB;
+  // 16-byte chunk x = 64 j + lane of a tile is chunk x % CH of token x / CH: its
+  // token's place in a table, and where in the row it lies (opaque, or both are worked out again for each tile)
+  uint32_t place[L::LOADS];
+#pragma unroll
+  for (int j = 0; j < L::LOADS; ++j) {
+    const int x = min(64 * j + lane, L::kChunks - 1);
+    place[j] = (uint32_t)(x / R::CH * 4) << 16 | (uint32_t)(x % R::CH * 16);
+    asm volatile("" : "+v"(place[j]));
+  }
+  auto load_tile = [&](int i) {
+    const int tile = tile0 + i * NW;
+    const uint32_t to = my + i % L::kBuf * L::kTileB, words = tab + (i & 3) * 256;
     int rows[L::LOADS];
 #pragma unroll
-    for (int i = 0; i < L::LOADS; ++i) {
-      const int r = min(64 * i + lane, L::kChunks - 1) / R::CH;
-      if (TAB && slots) rows[i] = (int)min(word_at(tab + (tile & 3) * 256 + r * 4), (uint32_t)a.own.pool_last);
-      else rows[i] = token(tile, r);
+    for (int j = 0; j < L::LOADS; ++j) {
+      if (TAB && slots) rows[j] = (int)min(word_at(words + (place[j] >> 16)), (uint32_t)a.own.pool_last);
+      else rows[j] = token(tile, (int)(place[j] >> 18));
     }
     wait_lds_reads();
+    auto all = [&](auto load) {
 #pragma unroll
-    for (int i = 0; i < L::LOADS; ++i) {
-      const int x = 64 * i + lane;
-      if (L::kChunks % 64 == 0 || x < L::kChunks) load_lds16(rows_of + rows[i] * row_bytes + x % R::CH * 16, to + i * 1024);
-    }
+      for (int j = 0; j < L::LOADS; ++j)
+        if (L::kChunks % 64 == 0 || 64 * j + lane < L::kChunks) load(j, place[j] & 0xFFFFu);
+    };
+    if (near) all([&](int j, uint32_t in) { load_lds16_near_once(rows_of, __umul24(rows[j], (uint32_t)row_bytes) + in, to + j * 1024); });
+    else all([&](int j, uint32_t in) { load_lds16_once(rows_of + (rows[j] * row_bytes + in), to + j * 1024); });
   };
 
   f32x4 o[JW];
@@ -128,8 +142,9 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_packed_narrow_kernel(Attend
   for (int j = 0; j < JW; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = 0.f;
   bool large = false;                        // a row's m is: see kLargeRef
-  auto compute = [&](int tile) {
-    const uint32_t buf = my + tile % L::kBuf * L::kTileB;
+  auto compute = [&](int i) {
+    const int tile = tile0 + i * NW;
+    const uint32_t buf = my + i % L::kBuf * L::kTileB;
     f32x4 x[2];
 #pragma unroll
     for (int tb = 0; tb < 2; ++tb) {
@@ -164,7 +179,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_packed_narrow_kernel(Attend
           bool vis = u < rg.cnt;
           if (!one) {
             int pt;
-            if (TAB && poss) pt = (int)word_at(tab + (tile & 3) * 256 + 128 + (16 * tb + 4 * q + r) * 4);
+            if (TAB && poss) pt = (int)word_at(tab + (i & 3) * 256 + 128 + (16 * tb + 4 * q + r) * 4);
             else pt = rg.token(min(u, rg.cnt - 1));
             vis = vis && sees(pt, qp, a.window, a.n_sink);
           }
@@ -202,9 +217,9 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_packed_narrow_kernel(Attend
         const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[tb][r], sl2, -ref));
         const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[tb][r + 1], sl2, -ref));
         lt += p0 + p1;
-        const uint16_t h0 = to_elem<true>(p0), h1 = to_elem<true>(p1);
-        ph[2 * tb + r / 2] = h0 | (uint32_t)h1 << 16;
-        if constexpr (F16) pl[2 * tb + r / 2] = to_elem<true>(p0 - elem<true>(h0)) | (uint32_t)to_elem<true>(p1 - elem<true>(h1)) << 16;
+        const uint32_t w = pack2<true>(p0, p1);
+        ph[2 * tb + r / 2] = w;
+        if constexpr (F16) pl[2 * tb + r / 2] = pack2<true>(p0 - half_of(w, 0), p1 - half_of(w, 1));
       }
     l += lt;
     // words of two tokens: codes of even widths (lo) and of odd ones (hi)
@@ -242,37 +257,35 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_packed_narrow_kernel(Attend
     }
   };
 
-  // loads of tiles t + 1 and t + 2 and the table of tile t + 3 are under way during tile t
+  // tile i + 1 and the table of tile i + 2 are loaded during tile i
   constexpr int KV = L::LOADS, T = TAB ? 1 : 0;
-  if (tile0 < tile1) {
+  if (my_tiles) {
     // From here on the wave counts its loads itself: what the compiler loaded
     // has to have arrived, or its own waits inside the loop would drain them.
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qf[ks]));
     asm volatile("" : "+v"(qp), "+v"(row_sl2));
     wait_loads<0>();
-    load_tables(tile0);
-    if (tile0 + 1 < tile1) load_tables(tile0 + 1);
-    if (tile0 + 2 < tile1) load_tables(tile0 + 2);
+    load_tables(0);
+    if (1 < my_tiles) load_tables(1);
     if (TAB) wait_loads<0>();
-    load_tile(tile0);
-    if (tile0 + 1 < tile1) load_tile(tile0 + 1);
-    for (int t = tile0; t < tile1; ++t) {
-      // Under way, oldest first: tile(t), tables(t + 2), tile(t + 1).
-      if (t + 2 < tile1) {
-        if (t + 3 < tile1) {
-          load_tables(t + 3);
+    load_tile(0);
+    for (int i = 0; i < my_tiles; ++i) {
+      // Under way, oldest first: tables(i + 1), tile(i).
+      if (i + 1 < my_tiles) {
+        if (i + 2 < my_tiles) {
+          load_tables(i + 2);
           wait_loads<KV + T>();
         } else {
           wait_loads<KV>();
         }
-        load_tile(t + 2);
-      } else if (t + 1 < tile1) {
-        wait_loads<KV>();
+        load_tile(i + 1);
+        if (i + 2 < my_tiles) wait_loads<KV + T>();
+        else wait_loads<KV>();
       } else {
         wait_loads<0>();
       }
-      compute(t);
+      compute(i);
     }
   }
   wait_loads<0>();
@@ -298,7 +311,9 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_packed_narrow_kernel(Attend
       for (int j = 0; j < JW; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
       m = -INFINITY;
       l = 0.f;
-      for (int u = tile0 * L::kTok; u < min(tile1 * L::kTok, rg.cnt); ++u) {
+      for (int v = 0; v < my_tiles * L::kTok; ++v) {
+        const int u = (tile0 + v / L::kTok * NW) * L::kTok + v % L::kTok;
+        if (u >= rg.cnt) break;
         const int t = rg.token(u);
         const char* row = rows_of + (slots ? (int)min((uint32_t)slots[t], (uint32_t)a.own.pool_last) : t) * row_bytes;
         float x = 0.f;
@@ -337,7 +352,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attend_packed_narrow_kernel(Attend
     sm[wave][c] = m;
     sl[wave][c] = l;
   }
-  finish_block<D, F16, NW>(a, sp, PrefixParts{nullptr, nullptr, 0, 1}, it, r0, n_rows, g, tiles, L::kWaveB, sm, sl, last);
+  finish_block<D, F16, NW, true>(a, sp, PrefixParts{nullptr, nullptr, 0, 1}, it, r0, n_rows, g, tiles, L::kWaveB, sm, sl, last);
 }
 
 }  // namespace
@@ -346,7 +361,7 @@ hipError_t launch_packed_narrow(const AttendArgs& a, const AttendPlan& p, const 
   const dim3 grid((unsigned)p.grid);
   const bool tab = a.own.slot || a.own.pos;
 #define CKV_NARROW(D, F16, TAB) \
-  if (p.alone) attend_packed_narrow_kernel<D, F16, TAB, 8><<<grid, 512, 0, s>>>(a, sp, p.target, p.min_chunk, true); \
+  if (p.alone) attend_packed_narrow_kernel<D, F16, TAB, 12><<<grid, 768, 0, s>>>(a, sp, p.target, p.min_chunk, true); \
   else attend_packed_narrow_kernel<D, F16, TAB, 4><<<grid, 256, 0, s>>>(a, sp, p.target, p.min_chunk, false)
 #define CKV_NARROW2(D, F16) \
   if (tab) { CKV_NARROW(D, F16, true); } \

@@ -75,20 +75,6 @@ __device__ __forceinline__ f32x16 mfma32(u32x4 x, u32x4 y, f32x16 c) {
   else return mfma_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), c);
 }
 
-// two values rounded to the type, packed
-template <bool F16>
-__device__ __forceinline__ uint32_t pack2(float x, float y) {
-  typedef float f32x2 __attribute__((ext_vector_type(2)));
-  const f32x2 v = {x, y};
-  if constexpr (F16) {
-    typedef _Float16 h2 __attribute__((ext_vector_type(2)));
-    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, h2));
-  } else {
-    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
-    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, b2));
-  }
-}
-
 __device__ __forceinline__ void tile_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // ---------------------------------------------------------------- shares

@@ -47,8 +47,9 @@ template <int P>
 __device__ __forceinline__ uint32_t two_values(uint32_t w, const Scale& c) {
   constexpr int up = 6 - 4 * P;
   const uint32_t at = up > 0 ? w << (up > 0 ? up : 0) : w >> (up < 0 ? -up : 0);
-  const h2 n = __builtin_bit_cast(h2, (at & 0x03C003C0u) | 0x4C004C00u);
-  return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(n, c.s, c.b));
+  uint32_t n;      // (at & mask) | exponents: with both as literals the compiler takes two instructions
+  asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(n) : "v"(at), "s"(0x03C003C0u), "v"(0x4C004C00u));
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(__builtin_bit_cast(h2, n), c.s, c.b));
 }
 // the eight widths of a word, in their order
 __device__ __forceinline__ u32x4 eight_values(uint32_t w, const Scale& c) {
