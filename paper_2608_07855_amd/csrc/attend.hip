@@ -356,16 +356,30 @@ AttendPlan plan_narrow(const AttendArgs& a, int64_t max_tokens, bool room) {
   int64_t e = p.target / a.Hkv + blocks + 1;
   if (a.packed) {
     // Caches in 4 bits: 12 waves a compute unit either way, as one workgroup or as three.
-    // Many row blocks: twice as many splits as run at a time (64 long ragged sequences
-    // 290 us; with 1024 splits 310, with 3072 290).  Few: splits of 256 tokens for
-    // short caches, up to 16 of them (what is joined at once), 768 tokens for long
-    // ones (one cache of 8192 tokens 21.7 us, in 32 splits 27.7).  Caches up to 2048
-    // tokens stay whole where blocks are not few (16 of 1024 tokens 13.1 us, in halves 16.4; 4224: 30, whole 35).
-    if (!p.alone) p.target = 1536;
-    p.min_chunk = small ? (int)std::min<int64_t>(std::max<int64_t>(seen / 16, 256), 768) : p.alone ? 2048 : 1024;
-    e = p.target / a.Hkv + blocks + 1;
+    const int64_t likely = std::min(blocks, n_seq * (((int64_t)a.max_rows * a.group + 15) / 16)) * a.Hkv;
+    // Up to a block a compute unit each has a workgroup of 12 waves (32 caches of 4096
+    // tokens 36 us, as below 42; 2 row blocks each of 16 caches 46 and 65), unless
+    // lengths that may differ by much (32 of up to 32768) would leave most units waiting for a few.
+    p.alone = likely <= 256 && (likely <= 128 || seen <= 8192);
+    p.target = p.alone ? 256 : 1536;
+    // Few blocks: splits of 256 tokens for short caches, up to 16 of them (what is joined
+    // at once), 768 tokens for long ones (one cache of 8192 tokens 21.7 us, in 32 splits
+    // 27.7).  A block for half of the units: halves of 2048 tokens or more (16 caches of
+    // 1024 tokens whole 13.1 us, in halves 16.4; of 4224 tokens 35 and 29).  Many: twice as
+    // many splits as run at a time, of 4096 tokens or more (64 long ragged sequences whole
+    // 457 us, so 283, in half as many 310; 64 of 4096 tokens whole 69, in halves 79).
+    const bool few = likely <= 96;
+    p.min_chunk = few ? (int)std::min<int64_t>(std::max<int64_t>(seen / 16, 256), 768) : p.alone ? 2048 : 4096;
+    int64_t e = p.target / a.Hkv + blocks + 1;
+    if (!room || seen <= (few ? 512 : p.min_chunk) || (p.alone && likely > 128) || blocks * a.Hkv >= 4096) {
+      p.min_chunk = INT_MAX;
+      e = blocks;
+    }
+    p.items = p.grid = e * a.Hkv;
+    p.split = p.min_chunk != INT_MAX;
+    return p;
   }
-  if (!room || seen <= (small ? 512 : 2048) || blocks * a.Hkv >= 4096) {
+  if (!room || seen <= (small ? 512 : 2048) || blocks * a.Hkv >= 4 * p.target) {
     p.min_chunk = INT_MAX;                                              // no splits
     e = blocks;
   }
