@@ -817,10 +817,11 @@ int ckv_unpack_tokens(ckv_ctx* ctx, const ckv_packed_view* kv,
  * ckv_attend_window over packed caches.  dtype: of queries and outputs.  Keys and
  * values are the fp16 numbers that the codes stand for; which tokens a row sees,
  * outputs, hidden tokens, workspace, capture and errors are as there.
- * Precision: bf16 queries are taken as fp16 times a power of two of each row's own
- * (elements below 2^-29 of the row's largest lose bits, 2^-40 of it at most), softmax
- * weights are rounded once to fp16 as there (for fp16 outputs of few rows: weight
- * and rest); float32 logits, maxima, sums and accumulation.
+ * Precision: bf16 queries are taken as fp16 times a power of two, one for each
+ * row where few rows read a cache, else for up to 32 rows of a sequence: elements
+ * below 2^-29 of the largest finite one of these are off by 2^-40 of it at most.
+ * Softmax weights are rounded once to fp16 as there (for fp16 outputs of few rows:
+ * weight and rest); float32 logits, maxima, sums and accumulation.
  */
 int ckv_attend_packed(ckv_ctx* ctx, const ckv_packed_view* kv,
                       const ckv_query_view* q, int32_t dtype, int32_t window,

@@ -69,7 +69,15 @@ __global__ __launch_bounds__(64 * NW, 3) void attend_packed_narrow_kernel(Attend
     for (int ks = 0; ks < KS; ++ks) qf[ks] = ldg_u4(qr + D / 4 * q + 8 * ks);
   }
   float row_sl2 = a.sl2;
-  if constexpr (!F16) row_sl2 *= queries_to_f16<KS>(qf, [](float v) { return max_rows16(v); });
+  if constexpr (!F16) {
+    float most = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) most = largest_finite(qf[ks], most);
+    const PowerOfTwo f = factor_of(max_rows16(most));
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = to_f16(qf[ks], f.mul);
+    row_sl2 *= f.back;
+  }
   const bool one = p_first == p_last;        // one position: what is loaded is what is seen
   int qmin = qp, qmax = qp;
   if (!one) {
@@ -240,8 +248,10 @@ __global__ __launch_bounds__(64 * NW, 3) void attend_packed_narrow_kernel(Attend
     }
     auto value = [&](auto P) {
       constexpr int pp = decltype(P)::value;
-      const u32x4 even = {two_values<pp>(lo[0], sc[0]), two_values<pp>(lo[1], sc[1]), two_values<pp>(lo[2], sc[2]), two_values<pp>(lo[3], sc[3])};
-      const u32x4 odd = {two_values<pp>(hi[0], sc[0]), two_values<pp>(hi[1], sc[1]), two_values<pp>(hi[2], sc[2]), two_values<pp>(hi[3], sc[3])};
+      auto values = [&](const uint32_t (&w)[4]) {
+        return values_of(two_codes<pp>(w[0]), two_codes<pp>(w[1]), two_codes<pp>(w[2]), two_codes<pp>(w[3]), sc[0], sc[1], sc[2], sc[3]);
+      };
+      const u32x4 even = values(lo), odd = values(hi);
       o[2 * pp] = mfma16<true>(even, ph, o[2 * pp]);
       o[2 * pp + 1] = mfma16<true>(odd, ph, o[2 * pp + 1]);
       if constexpr (F16) {

@@ -244,7 +244,7 @@ __device__ __forceinline__ const AttendArgs& fresh_args(const AttendArgs&) {
 }
 
 enum Kept { kS, kRb, kR0, kRows, kX0, kX1 = kX0 + 2, kWork = kX1 + 2, kQmin = kWork + 2, kQmax, kBmin, kBmax, kNextS, kNextRb,
-            kNextX, kLeft = kNextX + 2, kOpening = kLeft + 2, kRecord };
+            kNextX, kLeft = kNextX + 2, kOpening = kLeft + 2, kRecord, kBack = kRecord + 4, kKept };
 
 // PRE: the rows of all sequences over the shared tokens, in n_split splits, as
 // partial sums.  Otherwise a share of the blocks (W shares a KV head), in each
@@ -252,13 +252,15 @@ enum Kept { kS, kRb, kR0, kRows, kX0, kX1 = kX0 + 2, kWork = kX1 + 2, kQmin = kW
 //
 // PACK: caches in 4 bits.  Direct loads bring a wave's rows of a tile to LDS as they
 // are; two tiles before their products the wave makes fp16 of them and writes
-// them where a 16-bit tile would have been loaded, for all waves: a 256th of the
-// block's rows' work a token instead of one in each wave.  All products are fp16;
-// bf16 queries become fp16 times a power of two of their row's own.
+// them where a 16-bit tile would have been loaded, for all waves, so that a token is made
+// once for 256 rows.  That goes on between the products with the values (chunks of 8
+// prompts 693 us with a tile made before each step, 658 so).  All products are fp16;
+// bf16 queries become fp16 times a power of two of their wave's 32 rows.
 template <int D, bool F16, bool TAB, bool PRE, bool PACK>
 __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, SplitSpace sp, int W, int n_split) {
   using L = Wide<D>;
   constexpr bool C16 = F16 || PACK;        // what the products take
+  constexpr bool kFactor = PACK && !F16;   // queries were scaled
   constexpr int KS = D / 16, DB = D / 32;
   __shared__ __align__(256) char tiles[L::kLds + (PACK ? kNW * 4 * L::kRawB : 0)];
   __shared__ ShareShared ssh;
@@ -266,6 +268,7 @@ __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, Sp
   // What a block needs again behind its tiles waits in LDS (a copy a wave), and
   // the arguments are read anew: kept in scalar registers through the tiles they
   // spill, and a spilled register's reload inside the loop drains the loads.
+  static_assert(kKept <= 32);
   __shared__ volatile int kept[kNW][32];
   // (One block, and no second part, leave registers enough: PRE keeps both.)
   auto fresh = [&]() -> const AttendArgs& {
@@ -360,8 +363,20 @@ __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, Sp
     const uint16_t* qr = a.q + (int64_t)(r0 + p) * a.q_row_stride + (int64_t)h * a.q_head_stride;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) qf[ks] = ldg_u4(qr + 16 * ks + 8 * hf);
-    float back = 1.f;             // the row's logits are its products times this
-    if constexpr (PACK && !F16) back = queries_to_f16<KS>(qf, [](float v) { return max32(v); });
+    if constexpr (kFactor) {
+      // the wave's logits are its products times one factor (one for each row would take a
+      // vector register that the tiles' loop does not have)
+      float most = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) most = largest_finite(qf[ks], most);
+      most = max32(most);
+#pragma unroll
+      for (int off = 16; off; off >>= 1) most = fmaxf(most, __shfl_xor(most, off, 64));
+      const PowerOfTwo f = factor_of(most);
+      keep(kBack, (int)__float_as_uint(f.back));
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) qf[ks] = to_f16(qf[ks], f.mul);
+    }
     int qmin = qp, qmax = qp;
 #pragma unroll
     for (int off = 16; off; off >>= 1) {
@@ -470,7 +485,8 @@ __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, Sp
       const AttendArgs& a = fresh();
       const SeqCaches& kv = k ? a.own : a.pre;
       const Part pt = open(k);
-      const float sl2 = a.sl2 * back;
+      float sl2 = a.sl2;
+      if constexpr (kFactor) sl2 = __uint_as_float(uniform((int)__float_as_uint(sl2 * __uint_as_float(get(kBack)))));
       const Range rg = pt.rg;
       const int tile0 = pt.tile0, tile1 = pt.tile1;
       const int64_t head = g * kv.head_stride + (kv.slot ? 0 : pt.sq * kv.seq_stride);
@@ -549,28 +565,31 @@ __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, Sp
           else load_lds16(kh + ((uint64_t)rows[j] * row_bytes + in), to + j * 1024);
         }
       };
-      // eight lanes a row: lane i % 8 has widths D/4 (i % 4) .. of its key (i % 8 < 4) or value
-      auto make_tile = [&](int tile) {
+      // Eight lanes a row: lane i % 8 has widths D/4 (i % 4) .. of its key (i % 8 < 4) or
+      // value, in D / 32 words.
+      struct Made {
+        uint32_t from, to, params;
+      };
+      const auto word = [](uint32_t at) { return *(const __attribute__((address_space(3))) uint32_t*)(uintptr_t)at; };
+      auto make_begin = [&](int tile) {
         int ln = lane;
         asm volatile("" : "+v"(ln));
         const int row = ln >> 3, part = ln & 3, value = (ln >> 2) & 1, r = wave * L::kOwn + row;
         const uint32_t from = raw + (tile & 3) * L::kRawB + row * R::kBytes;
-        const auto word = [](uint32_t at) { return *(const __attribute__((address_space(3))) uint32_t*)(uintptr_t)at; };
-        const Scale sc = scale_of(word(from + R::kParams + value * (D / 8) + D / 4 * part / 32 * 4));
-        uint32_t w[D / 32];
-        const uint32_t at = from + value * R::kValue + D / 8 * part;
-        if constexpr (D == 128) {
-          const u32x4 c4 = lds_read16(at);
+        Made k;
+        k.from = from + value * R::kValue + D / 8 * part;
+        // (chunk D/32 part + i of the row lies at this ^ 16 i)
+        k.to = lds + (value * 3 + tile % 3) * L::kTileB + r * L::kRowB + ((D / 32 * part ^ (r << value & (L::CH - 1))) << 4);
+        k.params = word(from + R::kParams + value * (D / 8) + D / 4 * part / 32 * 4);
+        return k;
+      };
+      auto make_word = [&](const Made& k, int i, uint32_t codes) {
+        *(__attribute__((address_space(3))) u32x4*)(uintptr_t)(k.to ^ (i << 4)) = eight_values(codes, scale_of(k.params));
+      };
+      auto make_tile = [&](int tile) {
+        const Made k = make_begin(tile);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) w[i] = c4[i];
-        } else {
-          w[0] = word(at);
-          w[1] = word(at + 4);
-        }
-        const uint32_t to = lds + (value * 3 + tile % 3) * L::kTileB + r * L::kRowB, mix = (r << value) & (L::CH - 1);
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i)
-          *(__attribute__((address_space(3))) u32x4*)(uintptr_t)(to + (((D / 32 * part + i) ^ mix) << 4)) = eight_values(w[i], sc);
+        for (int i = 0; i < D / 32; ++i) make_word(k, i, word(k.from + 4 * i));
       };
 
       // scores of a tile (raw products)
@@ -678,6 +697,11 @@ __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, Sp
 #pragma unroll
           for (int j = 0; j < kAhead; ++j) vf[j] = read(j);
           my = -INFINITY;
+          // 4 bits: tile t + 2 is made here, where the vector units have least to do (past the
+          // last one from what an older tile left, for nobody)
+          Made made;
+          uint32_t codes;
+          if constexpr (PACK) made = make_begin(t + 2);
           __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
           for (int j = 0; j < 4 * DB; ++j) {
@@ -686,6 +710,10 @@ __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, Sp
 #pragma unroll
             for (int q = j * 16 / (4 * DB); q < (j + 1) * 16 / (4 * DB); ++q)
               my = max3(my, y[q / 8][2 * (q % 8)], y[q / 8][2 * (q % 8) + 1]);
+            if constexpr (PACK) {
+              if (j % 4 == 0) codes = word(made.from + j);
+              if (j % 4 == 3) make_word(made, j / 4, codes);
+            }
             __builtin_amdgcn_sched_barrier(0);
           }
         }
@@ -758,9 +786,9 @@ __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, Sp
                 wait_loads<0>();
               }
               if (t + 4 < tile1) load_raw(t + 4);
-              make_tile(t + 2);
             }
             if (wave_on) step(t, x, mx, y, my);
+            else if (t + 2 < tile1) make_tile(t + 2);
             return;
           }
           if (t + 3 < tile1) wait_loads<T + KV>();
@@ -858,7 +886,9 @@ __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, Sp
 #pragma unroll
             for (int j = 0; j < 8; ++j) x = fmaf(elem<C16>(chunk_elem(kk, j)), elem<C16>(chunk_elem(qf[ks], j)), x);
           }
-          x = product(sum32(x), b.sl2 * back);
+          float sl2 = b.sl2;
+          if constexpr (kFactor) sl2 *= __uint_as_float(get(kBack));
+          x = product(sum32(x), sl2);
           if (!(t < pt.row_hi && (t >= pt.row_lo || t < pt.rg.n_first))) continue;
           const float nm = fmaxf(m, x), ref = nm == -INFINITY ? 0.f : nm;
           const float al = __builtin_amdgcn_exp2f(m - ref), p = __builtin_amdgcn_exp2f(x - ref);

@@ -38,22 +38,33 @@ __device__ __forceinline__ Scale scale_of(uint32_t p0, uint32_t p1) {
           __builtin_bit_cast(h2, __builtin_amdgcn_perm(p1, p0, 0x07060302u))};
 }
 
-// Codes p of both halves of w as values, in fp16.  In the upper 4 of its 10
-// bits, behind the exponent of 16, a code n is the number 16 + n, exactly: a shift,
-// one instruction that masks and joins, and a fused product and sum make two
-// values.  (With a code at the low end of the mantissa, 1024 + n, the base would
-// be 64 times as far from the values, and its rounding with it.)
+// Codes p of both halves of w, shifted into the upper 4 of the 10 bits of an fp16 mantissa.
 template <int P>
-__device__ __forceinline__ uint32_t two_values(uint32_t w, const Scale& c) {
+__device__ __forceinline__ uint32_t two_codes(uint32_t w) {
   constexpr int up = 6 - 4 * P;
-  const uint32_t at = up > 0 ? w << (up > 0 ? up : 0) : w >> (up < 0 ? -up : 0);
-  uint32_t n;      // (at & mask) | exponents: with both as literals the compiler takes two instructions
-  asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(n) : "v"(at), "s"(0x03C003C0u), "v"(0x4C004C00u));
-  return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(__builtin_bit_cast(h2, n), c.s, c.b));
+  return up > 0 ? w << (up > 0 ? up : 0) : w >> (up < 0 ? -up : 0);
+}
+
+// Four such pairs as the values they stand for, in fp16.  Behind the exponent of 16 a
+// code n in those bits is the number 16 + n, exactly: one instruction that masks and
+// joins, and a fused product and sum make two values.  (With a code at the low end of
+// the mantissa, 1024 + n, the base would be 64 times as far from the values, and its
+// rounding with it.  In assembly, because the compiler takes two instructions where mask and
+// exponents are literals, and keeps them where the many-rows kernel has no registers if they are not; four
+// together, because it waits a cycle behind assembly.)
+__device__ __forceinline__ u32x4 values_of(uint32_t n0, uint32_t n1, uint32_t n2, uint32_t n3, const Scale& c0, const Scale& c1,
+                                           const Scale& c2, const Scale& c3) {
+  asm("v_and_or_b32 %0, %0, %4, %5\n\tv_and_or_b32 %1, %1, %4, %5\n\tv_and_or_b32 %2, %2, %4, %5\n\tv_and_or_b32 %3, %3, %4, %5"
+      : "+v"(n0), "+v"(n1), "+v"(n2), "+v"(n3)
+      : "s"(0x03C003C0u), "v"(0x4C004C00u));
+  const auto value = [](uint32_t n, const Scale& c) {
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(__builtin_bit_cast(h2, n), c.s, c.b));
+  };
+  return u32x4{value(n0, c0), value(n1, c1), value(n2, c2), value(n3, c3)};
 }
 // the eight widths of a word, in their order
 __device__ __forceinline__ u32x4 eight_values(uint32_t w, const Scale& c) {
-  return u32x4{two_values<0>(w, c), two_values<1>(w, c), two_values<2>(w, c), two_values<3>(w, c)};
+  return values_of(two_codes<0>(w), two_codes<1>(w), two_codes<2>(w), two_codes<3>(w), c, c, c, c);
 }
 
 // Widths 8j to 8j+7 of a key (or value) of a row in memory.
@@ -65,25 +76,29 @@ __device__ __forceinline__ u32x4 row_values(const char* row, bool value, int j) 
 // the fp16 number in one half of a word
 __device__ __forceinline__ float half_of(uint32_t w, int h) { return (float)__builtin_bit_cast(h2, w)[h]; }
 
-// A row's 8 KS elements of the lane as fp16 times a power of two that brings the
-// row's largest to [2^14, 2^15); returns the inverse.  max_row: over the lanes of a row.
-template <int KS, class Max>
-__device__ __forceinline__ float queries_to_f16(u32x4 (&qf)[KS], Max max_row) {
-  float m = 0.f;
+// bf16 queries as fp16 times a power of two that brings the largest finite element to [2^14, 2^15).
+__device__ __forceinline__ float largest_finite(u32x4 x, float m) {
 #pragma unroll
-  for (int ks = 0; ks < KS; ++ks)
+  for (int e = 0; e < 8; ++e) {
+    const float y = fabsf(bf16_bits_to_float(chunk_elem(x, e)));
+    m = fmaxf(m, y < INFINITY ? y : 0.f);
+  }
+  return m;
+}
+struct PowerOfTwo {
+  float mul, back;      // the factor and its inverse
+};
+__device__ __forceinline__ PowerOfTwo factor_of(float largest) {
+  const uint32_t ex = max(__float_as_uint(largest) >> 23, 15u);
+  return {__uint_as_float((268u - ex) << 23), __uint_as_float((ex - 14u) << 23)};
+}
+__device__ __forceinline__ u32x4 to_f16(u32x4 x, float mul) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(bf16_bits_to_float(chunk_elem(qf[ks], e))));
-  const uint32_t ex = max(__float_as_uint(max_row(m)) >> 23, 15u);
-  const float mul = __uint_as_float((268u - ex) << 23);
-#pragma unroll
-  for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const h2 v = {(_Float16)(bf16_bits_to_float(qf[ks][r] & 0xFFFFu) * mul), (_Float16)(__uint_as_float(qf[ks][r] & 0xFFFF0000u) * mul)};
-      qf[ks][r] = __builtin_bit_cast(uint32_t, v);
-    }
-  return __uint_as_float((ex - 14u) << 23);
+  for (int r = 0; r < 4; ++r) {
+    const h2 v = {(_Float16)(bf16_bits_to_float(x[r] & 0xFFFFu) * mul), (_Float16)(__uint_as_float(x[r] & 0xFFFF0000u) * mul)};
+    x[r] = __builtin_bit_cast(uint32_t, v);
+  }
+  return x;
 }
 
 }  // namespace
