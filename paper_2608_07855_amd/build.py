@@ -8,8 +8,8 @@ debug    paper_2608_07855_amd/libcommitkv_debug.so: the same sources with
          include/commitkv.h).
 asan     paper_2608_07855_amd/libcommitkv_asan.so: host code built with
          AddressSanitizer and UndefinedBehaviorSanitizer (device code as in
-         release), and _build/asan/abi_driver and serving_driver, programs
-         that run every C ABI entry point (tests/native/) against it.
+         release), and _build/asan/abi_driver, serving_driver and packed_driver,
+         programs that run every C ABI entry point (tests/native/) against it.
 
 Objects go to ``paper_2608_07855_amd/_build/<variant>``.
 """
@@ -48,6 +48,7 @@ VARIANTS = {
 LIB = os.path.join(PKG, VARIANTS["release"][0])
 DRIVER = os.path.join(BUILD_DIR, "asan", "abi_driver")
 SERVING_DRIVER = os.path.join(BUILD_DIR, "asan", "serving_driver")
+PACKED_DRIVER = os.path.join(BUILD_DIR, "asan", "packed_driver")
 # roctx ranges (rocprofiler-sdk's roctx library, part of every ROCm 7 install)
 LINK_LIBS = ["-L/opt/rocm/lib", "-lrocprofiler-sdk-roctx", "-Wl,-rpath,/opt/rocm/lib"]
 
@@ -86,7 +87,7 @@ def build(verbose: bool = False, variant: str = "release") -> str:
     if variant == "asan":
         # the drivers carry the sanitizer runtimes; they find the library
         # two directories up from themselves
-        for driver in (DRIVER, SERVING_DRIVER):
+        for driver in (DRIVER, SERVING_DRIVER, PACKED_DRIVER):
             name = os.path.basename(driver)
             _run([HIPCC, "-x", "hip", "--offload-arch=gfx950", "-O1", "-std=c++17", "-Wall",
                   "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", *HOST_SANITIZE,
