@@ -2075,7 +2075,7 @@ bool rows_apart(int64_t w, Axis (&&ax)[N]) {
   for (const Axis& x : ax)
     if (x.n > 1) {
       if (x.st < w) return false;
-      w += extent(x.n, x.st);
+      w = std::min(w + extent(x.n, x.st), INT64_MAX / 2);
     }
   return true;
 }

@@ -356,7 +356,7 @@ AttendPlan plan_narrow(const AttendArgs& a, int64_t max_tokens, bool room) {
   int64_t e = p.target / a.Hkv + blocks + 1;
   if (a.packed) {
     // Caches in 4 bits: 12 waves a compute unit either way, as one workgroup or as three.
-    const int64_t likely = std::min(blocks, n_seq * (((int64_t)a.max_rows * a.group + 15) / 16)) * a.Hkv;
+    const int64_t likely = std::min(blocks, n_seq * std::min(blocks, ((int64_t)a.max_rows * a.group + 15) / 16)) * a.Hkv;
     // Up to a block a compute unit each has a workgroup of 12 waves (32 caches of 4096
     // tokens 36 us, as below 42; 2 row blocks each of 16 caches 46 and 65), unless
     // lengths that may differ by much (32 of up to 32768) would leave most units waiting for a few.

@@ -11,7 +11,10 @@ namespace {
 constexpr int kNT = 256;
 constexpr int kMany = 4;                  // tokens of a thread that reads back, whose loads leave together, where a
 constexpr int kFew = 4096;                // launch has more than so many workgroups of one each (16 a compute unit)
-constexpr int64_t kGroups = 1 << 20;      // workgroups of a launch at most; each takes every so many items
+// Workgroups of a launch at most, each of which takes every so many items: calls whose
+// tables have far more room than tokens launch few that find nothing (4096 cost
+// one cache of 131072 tokens 10%).
+constexpr int64_t kGroups = 1 << 15;
 constexpr float kMostElem = 16384.f;   // b reaches -3.2 times this: inside fp16's range
 
 // of the lane beside it (lanes 2i and 2i + 1)
@@ -124,42 +127,45 @@ __global__ __launch_bounds__(kNT) void unpack_kernel(PackArgs a) {
   constexpr int LPT = D / 8, TPB = kNT / 2 / LPT;      // threads of a key or value, tokens of a workgroup at a time
   const bool value = threadIdx.x >= kNT / 2;           // a wave's stores lie together
   const int w8 = threadIdx.x % LPT, tok = threadIdx.x % (kNT / 2) / LPT;
-  const int64_t tiles = (a.max_tokens + TPB * U - 1) / (TPB * U), n_items = tiles * a.Hkv * a.n_seq;
-  for (int64_t item = blockIdx.x; item < n_items; item += gridDim.x) {
-    const int g = (int)(item / tiles % a.Hkv), s = (int)(item / tiles / a.Hkv), t0 = (int)(item % tiles) * (TPB * U) + tok;
+  // workgroup `group` of `groups` of a sequence and head, or of every so many of these
+  const int64_t pairs = (int64_t)a.Hkv * a.n_seq;
+  const int groups = (int)max((int64_t)gridDim.x / pairs, (int64_t)1), group = (int)(blockIdx.x % groups);
+  for (int64_t pair = blockIdx.x / groups; pair < pairs; pair += gridDim.x / groups) {
+    const int g = (int)(pair % a.Hkv), s = (int)(pair / a.Hkv);
     const int n = min(max(a.n_tokens[s], 0), a.max_tokens);
-    if (t0 - tok >= n) continue;
     const char* from = a.pool + (a.slot ? 0 : s * a.pool_seq) + g * a.pool_head;
-    int row[U];
+    for (int64_t first = (int64_t)group * (TPB * U); first < n; first += (int64_t)groups * (TPB * U)) {
+      const int t0 = (int)first + tok;
+      int row[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int t = min(t0 + u * TPB, n - 1);
-      row[u] = a.slot ? (int)min((uint32_t)a.slot[s * a.slot_stride + t], (uint32_t)a.pool_last) : t;
-    }
-    uint32_t word[U], par[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      word[u] = ldg_i32(from + row[u] * a.pool_row + (value ? R::kValue : 0) + 4 * w8);
-      par[u] = ldg_i32(from + row[u] * a.pool_row + (value ? R::kValueParams : R::kParams) + w8 / 4 * 4);
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int t = t0 + u * TPB;
-      if (t >= n) break;
-      u32x4 y = eight_values(word[u], scale_of(par[u]));
-      if constexpr (!F16) {
-#pragma unroll
-        for (int p = 0; p < 4; ++p) {
-          typedef float f32x2 __attribute__((ext_vector_type(2)));
-          typedef __bf16 b2 __attribute__((ext_vector_type(2)));
-          y[p] = __builtin_bit_cast(uint32_t, __builtin_convertvector(__builtin_convertvector(__builtin_bit_cast(h2, (uint32_t)y[p]), f32x2), b2));
-        }
+      for (int u = 0; u < U; ++u) {
+        const int t = min(t0 + u * TPB, n - 1);
+        row[u] = a.slot ? (int)min((uint32_t)a.slot[s * a.slot_stride + t], (uint32_t)a.pool_last) : t;
       }
-      __builtin_nontemporal_store(y, reinterpret_cast<u32x4*>((value ? a.v : a.k) + s * a.seq_stride + g * a.head_stride + t * a.tok_stride + 8 * w8));
+      uint32_t word[U], par[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        word[u] = ldg_i32(from + row[u] * a.pool_row + (value ? R::kValue : 0) + 4 * w8);
+        par[u] = ldg_i32(from + row[u] * a.pool_row + (value ? R::kValueParams : R::kParams) + w8 / 4 * 4);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int t = t0 + u * TPB;
+        if (t >= n) break;
+        u32x4 y = eight_values(word[u], scale_of(par[u]));
+        if constexpr (!F16) {
+#pragma unroll
+          for (int p = 0; p < 4; ++p) {
+            typedef float f32x2 __attribute__((ext_vector_type(2)));
+            typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+            y[p] = __builtin_bit_cast(uint32_t, __builtin_convertvector(__builtin_convertvector(__builtin_bit_cast(h2, (uint32_t)y[p]), f32x2), b2));
+          }
+        }
+        __builtin_nontemporal_store(y, reinterpret_cast<u32x4*>((value ? a.v : a.k) + s * a.seq_stride + g * a.head_stride + t * a.tok_stride + 8 * w8));
+      }
     }
   }
 }
-
 
 }  // namespace
 
@@ -182,9 +188,11 @@ hipError_t launch_pack(const PackArgs& a, hipStream_t s) {
 
 hipError_t launch_unpack(const PackArgs& a, hipStream_t s) {
   const int tpb = kNT / (a.D / 4);
-  auto items = [&](int step) { return ((int64_t)a.max_tokens + step - 1) / step * a.Hkv * a.n_seq; };
-  const bool many = items(tpb) > kFew;
-  const dim3 grid((unsigned)std::min<int64_t>(kGroups, items(many ? kMany * tpb : tpb)));
+  const int64_t pairs = (int64_t)a.Hkv * a.n_seq;
+  auto tiles = [&](int step) { return ((int64_t)a.max_tokens + step - 1) / step; };
+  const bool many = tiles(tpb) * pairs > kFew;
+  // whole groups of workgroups for each sequence and head, or one for several of them
+  const dim3 grid((unsigned)std::min(kGroups, pairs * std::min(tiles(many ? kMany * tpb : tpb), std::max<int64_t>(kGroups / pairs, 1))));
   if (many) {
     CKV_PACKED(unpack_kernel, CKV_AND kMany)
   } else {

@@ -314,3 +314,33 @@ def test_refusals(ckv):
             assert code(P.ckv_unpack_tokens, bad, k=out[0], v=out[1]) == want, field
     ctx.sync()
     assert torch.all(pool == KEEP) and not any(x.any() for x in out)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_more_than_a_launch_of_items(ckv, d):
+    """More (sequence, head) pairs and tiles of tokens than workgroups; far more room than tokens."""
+    P, ctx = ckv
+    rng = np.random.default_rng(11)
+    n, hkv = 9001, 64                                # 9001 sequences of 64 heads, up to 2 tokens each
+    lens = rng.integers(0, 3, n)
+    rows = int(lens.sum())
+    g = torch.Generator().manual_seed(1)
+    k, v = (torch.randn((rows, hkv, d), generator=g).to(torch.bfloat16) for _ in range(2))
+    pool = torch.zeros((hkv, rows, O.row_bytes(d)), dtype=torch.uint8, device="cuda")
+    P.ckv_pack_tokens(ctx, k.cuda(), v.cuda(), _dev(np.arange(rows)), pool)
+    slot = np.zeros((n, 40), np.int64)
+    first = np.cumsum(lens) - lens
+    slot[:, 0], slot[:, 1] = first, first + 1
+    out = P.ckv_unpack_tokens(ctx, P.packed_view(pool, _dev(lens), slot=_dev(slot)),
+                              k=torch.full((n, hkv, 40, d), 9.0, dtype=torch.bfloat16, device="cuda"),
+                              v=torch.full((n, hkv, 40, d), 9.0, dtype=torch.bfloat16, device="cuda"))
+    ctx.sync()
+    some = rng.choice(rows, 200, replace=False)
+    assert np.array_equal(pool[:, torch.from_numpy(some).cuda()].cpu().numpy().transpose(1, 0, 2),
+                          O.pack(k[some].float().numpy(), v[some].float().numpy()))
+    seq = np.repeat(np.arange(n), lens)
+    want = O.unpack(pool.cpu().numpy())
+    for name, x in zip("kv", want):
+        got = out[name][torch.from_numpy(seq).cuda(), :, torch.from_numpy(np.arange(rows) - first[seq]).cuda()].cpu()
+        assert torch.equal(got, torch.from_numpy(x).to(torch.bfloat16).transpose(0, 1))
+        assert torch.all(out[name][:, :, 2:] == 9) and torch.all(out[name][torch.from_numpy(lens == 0).cuda()] == 9)
