@@ -289,10 +289,13 @@ def packed_row_bytes(head_dim: int) -> int:
     return head_dim // 4 * 5
 
 
+_PACKED_ROWS = {packed_row_bytes(d): d for d in (64, 128)}
+
+
 def _check_packed(pool, name, ndim):
     _check_dev(pool, name, torch.uint8, ndim)
-    if pool.shape[-1] not in (packed_row_bytes(64), packed_row_bytes(128)):
-        raise ValueError(f"{name}: rows of {pool.shape[-1]} bytes; a packed row has {packed_row_bytes(64)} or {packed_row_bytes(128)}")
+    if pool.shape[-1] not in _PACKED_ROWS:
+        raise ValueError(f"{name}: rows of {pool.shape[-1]} bytes; a packed row has {' or '.join(map(str, _PACKED_ROWS))}")
 
 
 def packed_view(pool, n_tokens, *, slot=None, pos=None, max_tokens: int | None = None) -> PackedView:
@@ -324,7 +327,7 @@ def packed_view(pool, n_tokens, *, slot=None, pos=None, max_tokens: int | None =
     view = PackedView(pool.data_ptr(), st[0] if slot is None else 0, st[-3], st[-2],
                       None if slot is None else slot.data_ptr(), 0 if slot is None else slot.stride(0),
                       None if pos is None else pos.data_ptr(), 0 if pos is None else pos.stride(0), n_tokens.data_ptr(), n,
-                      most, 0 if slot is None else pool.shape[-2], pool.shape[-3], pool.shape[-1] // 5 * 4)
+                      most, 0 if slot is None else pool.shape[-2], pool.shape[-3], _PACKED_ROWS[pool.shape[-1]])
     view._keep = (pool, n_tokens, slot, pos)   # the struct holds raw pointers: keep the tensors alive
     view._device = pool.device
     return view
@@ -652,15 +655,19 @@ def ckv_build_slots(ctx: Context, step: SlotStep):
     return step._out
 
 
-def _check_rows_16(ctx, k, v, ndim, pool_device):
+def _check_rows_16(ctx, k, v, ndim, device):
+    """Keys and values in 16 bits beside a pool on ``device``; their type as the C ABI has it.  (These calls last 3 us
+    on the device, so what is checked again for v is that it is like k.)"""
     if k.dtype not in _DTYPES:
         raise ValueError("k: expected bfloat16 or float16")
-    _check_dev(k, "k", k.dtype, ndim, pool_device)
-    _check_dev(v, "v", k.dtype, ndim, pool_device)
+    _check_dev(k, "k", k.dtype, ndim, device)
+    if v.dtype != k.dtype or v.device != device:
+        raise ValueError("v: expected a tensor of k's type and device")
     if k.shape != v.shape or k.stride() != v.stride():
         raise ValueError("k and v must have the same shape and strides")
-    if pool_device.index != ctx.device:
-        raise ValueError(f"the tensors are on {pool_device}, the context on device {ctx.device}")
+    if device.index != ctx.device:
+        raise ValueError(f"the tensors are on {device}, the context on device {ctx.device}")
+    return _DTYPES[k.dtype]
 
 
 def ckv_pack_tokens(ctx: Context, k, v, row, pool, *, n_live=None):
@@ -669,17 +676,18 @@ def ckv_pack_tokens(ctx: Context, k, v, row, pool, *, n_live=None):
     (uint8 [Hkv, pool_rows, packed_row_bytes(d)]).  Tokens from n_live[0] on (int32 [1], device;
     None: all live) and tokens whose row lies outside the pool are left out; the rows of
     the others must differ."""
+    device = pool.device
     _check_packed(pool, "pool", 3)
-    _check_rows_16(ctx, k, v, 3, pool.device)
-    n, hkv, d = k.shape
-    if hkv != pool.shape[0] or packed_row_bytes(d) != pool.shape[2]:
-        raise ValueError(f"the pool has {pool.shape[0]} heads and rows of {pool.shape[2]} bytes, the tokens {hkv} and "
-                         f"{packed_row_bytes(d)}")
-    _check_flat(row, "row", n, pool.device)
+    dtype = _check_rows_16(ctx, k, v, 3, device)
+    (n, hkv, d), (heads, pool_rows, row_bytes) = k.shape, pool.shape
+    if hkv != heads or packed_row_bytes(d) != row_bytes:
+        raise ValueError(f"the pool has {heads} heads and rows of {row_bytes} bytes, the tokens {hkv} and {packed_row_bytes(d)}")
+    _check_flat(row, "row", n, device)
     if n_live is not None:
-        _check_flat(n_live, "n_live", 1, pool.device)
-    rows = KVRows(k.data_ptr(), v.data_ptr(), 0, k.stride(1), k.stride(0), _DTYPES[k.dtype])
-    to = PackedPool(pool.data_ptr(), pool.stride(0), pool.stride(1), pool.shape[1], hkv, d)
+        _check_flat(n_live, "n_live", 1, device)
+    st, pt = k.stride(), pool.stride()
+    rows = KVRows(k.data_ptr(), v.data_ptr(), 0, st[1], st[0], dtype)
+    to = PackedPool(pool.data_ptr(), pt[0], pt[1], pool_rows, hkv, d)
     ctx.check(ctx._lib.ckv_pack_tokens(ctx.handle, ctypes.byref(rows), row.data_ptr(), _int32(n, "n"),
                                        None if n_live is None else n_live.data_ptr(), ctypes.byref(to)))
     return pool
@@ -689,15 +697,17 @@ def ckv_unpack_tokens(ctx: Context, kv: PackedView, *, k=None, v=None, dtype=tor
     """The keys and values that packed caches stand for: k, v [n_seq, Hkv, max_tokens, d]
     (or more tokens) of ``dtype``, unless given.  Rows past a sequence's tokens keep what they held
     (zeros where they are allocated here)."""
-    shape = (kv.n_seq, kv.n_kv_heads, kv.max_tokens, kv.head_dim)
     if (k is None) != (v is None):
         raise ValueError("k and v are given both or not at all")
     if k is None:
+        shape = (kv.n_seq, kv.n_kv_heads, kv.max_tokens, kv.head_dim)
         k, v = (torch.zeros(shape, dtype=dtype, device=kv._device) for _ in range(2))
-    _check_rows_16(ctx, k, v, 4, kv._device)
-    if (k.shape[0], k.shape[1], k.shape[3]) != (shape[0], shape[1], shape[3]) or k.shape[2] < shape[2]:
-        raise ValueError(f"k and v: expected {shape} or more tokens, not {tuple(k.shape)}")
-    out = KVRows(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2), _DTYPES[k.dtype])
+    kind = _check_rows_16(ctx, k, v, 4, kv._device)
+    n, hkv, most, d = k.shape
+    if n != kv.n_seq or hkv != kv.n_kv_heads or d != kv.head_dim or most < kv.max_tokens:
+        raise ValueError(f"k and v: expected {(kv.n_seq, kv.n_kv_heads, kv.max_tokens, kv.head_dim)} or more tokens, not {tuple(k.shape)}")
+    st = k.stride()
+    out = KVRows(k.data_ptr(), v.data_ptr(), st[0], st[1], st[2], kind)
     ctx.check(ctx._lib.ckv_unpack_tokens(ctx.handle, ctypes.byref(kv), ctypes.byref(out)))
     return dict(k=k, v=v)
 
