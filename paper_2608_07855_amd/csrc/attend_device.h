@@ -469,7 +469,7 @@ __device__ __forceinline__ float sum_rows16(float v) {
 // the waves, and over the block's splits by the one that finishes last.  TREE: of
 // more than 16 splits each 16 are joined first, by whichever finishes last of
 // them, and these sums by the last of those (a split's sums are 8 KB and more, which one
-// workgroup reads at 0.4 us a split: 256 splits of one cache 131 us, in a tree %TREE%).
+// workgroup reads at 0.4 us a split: one cache of 65536 tokens in 256 splits 131 us, in a tree 29).
 template <int D, bool F16, int NW, bool TREE = false>
 __device__ __forceinline__ void finish_block(const AttendArgs& a, const SplitSpace& sp, const PrefixParts& pp, const Item& it, int r0,
                                              int n_rows, int g, const char* tiles, int wave_bytes, const float (&sm)[NW][kNarrowRows],

@@ -27,6 +27,13 @@ namespace {
 //
 // bf16 queries become fp16 times a power of two of their row's own, which its logits
 // are divided by again: their 8 bits fit, and the largest lies below 2^15.
+//
+// Bound: HBM, and latency where there are few tiles a wave.  A tile is 5 KB (16 KB in 16
+// bits) and takes about 270 vector instructions, 1100 of the 2500 cycles or so in which its
+// bytes arrive on a loaded device, so waves count more than bytes under way: two buffers
+// and 12 waves a compute unit (LDS holds no more), 64 long ragged sequences 318 us, three
+// buffers and 8 waves 337; the loads alone take 279 either way, past the caches 251, and
+// then the whole 283 (5.3 TB/s; in 16 bits 862 us).
 // ---------------------------------------------------------------------------
 template <int D, int NW_>
 struct PackedNarrow {
