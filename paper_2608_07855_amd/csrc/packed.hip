@@ -96,7 +96,7 @@ __global__ __launch_bounds__(kNT) void pack_kernel(PackArgs a) {
     uint32_t word[2] = {0, 0};
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      const float y = (x[e] - bf) - s16;
+      const float y = (__builtin_amdgcn_fmed3f(x[e], -kMostElem, kMostElem) - bf) - s16;     // (there b is rounded by up to 8, a narrow group's steps)
       const float m = __builtin_amdgcn_fmed3f(floorf(__builtin_fmaf(y, inv, 0.5f - 0x1p-12f)), 0.f, 14.f);
       const uint32_t n = (uint32_t)m + (__builtin_fmaf(-m, sf, y) >= border ? 1u : 0u);
       word[e / 8] |= n << (4 * (e % 8 / 2) + 16 * (e % 2));
