@@ -22,7 +22,7 @@ def quantise(x):
     g = np.clip(np.where(whole[..., None], g, 0), np.float32(-16384), np.float32(16384))
     m, M = g.min(-1), g.max(-1)
     s = ((M - m) / np.float32(15)).astype(np.float16)
-    b = (m - np.float32(16) * s.astype(np.float32) + np.float32(0)).astype(np.float16)       # + 0: no negative zero
+    b = (m - np.float32(16) * s.astype(np.float32)).astype(np.float16) + np.float16(0)       # + 0: no negative zero
     t = (g - b.astype(np.float32)[..., None]).astype(np.float64)
     n = np.zeros(g.shape, np.int64)
     for k in range(1, 16):                            # the largest k whose border does not lie above t

@@ -86,11 +86,14 @@ __global__ __launch_bounds__(kNT) void pack_kernel(PackArgs a) {
     hi = fminf(fmaxf(hi, -kMostElem), kMostElem);
     constexpr float k15 = 1.f / 15.f;
     const float range = hi - lo, q = range * k15;
+    // (both are rounded to float32 first, and not by one instruction to fp16)
     float step = __builtin_fmaf(__builtin_fmaf(-15.f, q, range), k15, q);
-    asm("" : "+v"(step));                      // rounded to float32 first, and not by one instruction to fp16
+    asm("" : "+v"(step));
     _Float16 s = (_Float16)step;
     const float sf = (float)s;
-    _Float16 b = (_Float16)(__builtin_fmaf(-16.f, sf, lo) + 0.f);      // (a zero is +0, whatever signs the group's have)
+    float base = __builtin_fmaf(-16.f, sf, lo);
+    asm("" : "+v"(base));
+    _Float16 b = (_Float16)base + (_Float16)0.f;       // (a zero is +0, whatever its sign was before or behind the rounding)
     const float bf = (float)b, s16 = 16.f * sf;
     const float inv = sf > 0.f ? __builtin_amdgcn_rcpf(sf) : 0.f, border = sf > 0.f ? 0.5f * sf : INFINITY;
     uint32_t word[2] = {0, 0};

@@ -46,3 +46,13 @@ def test_groups_at_the_largest_elements(ckv, spread, d, type):
     k[0, 0, 3], v[0, 0, 40], k[1], v[1] = 16400, -60000, 16400, -16400
     k[2, 0, ::2], v[2, 0, 1::2], v[3] = torch.finfo(TYPES[type]).max, torch.finfo(TYPES[type]).min, 50000
     assert np.array_equal(_packed(ckv, k, v), O.pack(k.float().numpy(), v.float().numpy()))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_zero_base_has_no_sign(ckv, d):
+    """Groups of -0, and of tiny negative numbers whose base rounds to zero, hold +0 (all bytes 0)."""
+    k = torch.tensor([-0.0, -1e-8, -2.0**-25, -1e-30], dtype=torch.bfloat16).view(4, 1, 1).expand(4, 1, d).contiguous()
+    v = k.clone()
+    v[:, :, ::3] = 0.0                    # both zeros in a group
+    got = _packed(ckv, k, v)
+    assert np.array_equal(got, O.pack(k.float().numpy(), v.float().numpy())) and not got.any()

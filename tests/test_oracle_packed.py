@@ -35,6 +35,13 @@ def test_constant_and_far_groups():
     assert np.all(np.isfinite(O.values(n, [s], [b]))) and n[0] == 15 and n[1] == 0
 
 
+def test_a_zero_base_has_no_sign():
+    """-0, and what rounds to it: fp16's smallest number is 2^-24, a half of it or less is 0."""
+    for c in (-0.0, -1e-8, -2.0**-25, -1e-30):
+        n, s, b = O.quantise_group(np.full(32, c, np.float32))
+        assert s == 0 and b == 0 and not np.signbit(b) and not n.any()
+
+
 @pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
 def test_non_finite_group(bad):
     n, s, b = O.quantise_group(_group(1, bad))
