@@ -36,20 +36,48 @@ def version() -> int:
 
 
 class Context:
-    """A ckv_ctx bound to one device and one HIP stream (default: torch's current)."""
+    """A ckv_ctx bound to one device and one HIP stream (default: torch's current).  Outputs that a call
+    allocates belong to that stream; who gives tensors that another stream writes, or reads outputs on
+    another, orders the two."""
 
     def __init__(self, device: int = 0, stream=None):
         self._lib = lib()
         if stream is None:
-            stream = torch.cuda.current_stream(device).cuda_stream
-        elif isinstance(stream, torch.cuda.Stream):
-            stream = stream.cuda_stream
+            stream = torch.cuda.current_stream(device)
         self.device = device
+        self._bind(stream)
         h = ctypes.c_void_p()
-        rc = self._lib.ckv_create(ctypes.byref(h), device, ctypes.c_void_p(stream))
+        rc = self._lib.ckv_create(ctypes.byref(h), device, ctypes.c_void_p(self.stream))
         if rc != 0:
             raise CKVError(rc, "ckv_create failed")
         self.handle = h
+
+    def _bind(self, stream):
+        if isinstance(stream, torch.cuda.Stream):
+            self.stream, self._torch_stream = stream.cuda_stream, stream
+        else:
+            self.stream, self._torch_stream = int(stream or 0), None
+
+    def _outputs(self):
+        """new(shape, dtype, make): a tensor for a call's output.  Its memory is the context's stream's: on torch's current
+        one, memory that work under way there still uses could come back from the allocator, and a fill would
+        run beside the call's kernels."""
+        dev = torch.device("cuda", self.device)
+        here = torch.cuda.current_stream(dev)
+
+        def new(shape, dtype=torch.float32, make=torch.empty):
+            return make(shape, dtype=dtype, device=dev)
+        if here.cuda_stream == self.stream:
+            return new
+        if self._torch_stream is None:
+            self._torch_stream = torch.cuda.ExternalStream(self.stream, dev) if self.stream else torch.cuda.default_stream(dev)
+
+        def apart(shape, dtype=torch.float32, make=torch.empty):
+            with torch.cuda.stream(self._torch_stream):
+                t = new(shape, dtype, make)
+            t.record_stream(here)                # (where the caller will read it: it is not given out again before)
+            return t
+        return apart
 
     def check(self, rc: int):
         if rc != 0:
@@ -62,6 +90,7 @@ class Context:
     def set_stream(self, stream):
         s = stream.cuda_stream if isinstance(stream, torch.cuda.Stream) else stream
         self.check(self._lib.ckv_set_stream(self.handle, ctypes.c_void_p(s)))
+        self._bind(stream)
 
     def set_workspace_limit(self, nbytes: int):
         self.check(self._lib.ckv_set_workspace_limit(self.handle, nbytes))
@@ -406,13 +435,6 @@ def slot_step(n_tokens, n_new, free, n_free, slot, *, block_size: int, block_tab
     return step
 
 
-def _f32(n, device, fill=None):
-    t = torch.empty(n, dtype=torch.float32, device=device)
-    if fill is not None:
-        t.fill_(fill)
-    return t
-
-
 # ---------------------------------------------------------------- calls
 
 def ckv_measure_page_effects(ctx: Context, kv: KVView, win: WindowView, pages: Pages, *,
@@ -422,18 +444,18 @@ def ckv_measure_page_effects(ctx: Context, kv: KVView, win: WindowView, pages: P
     outputs to allocate when not given: "R_head", "o", "lse", "token_mass".
     ``noalloc`` calls ckv_measure_page_effects_noalloc (the library allocates
     nothing; outputs are still allocated here unless given)."""
-    dev = torch.device("cuda", ctx.device)
+    new = ctx._outputs()
     Hq, W, d = win.n_q_heads, win.n_rows, kv.head_dim
     if R is None:
-        R = _f32(max(pages.n, 1), dev)
+        R = new(max(pages.n, 1))
     if R_head is None and "R_head" in want:
-        R_head = _f32(max(pages.n * Hq, 1), dev)
+        R_head = new(max(pages.n * Hq, 1))
     if o is None and "o" in want:
-        o = _f32(Hq * W * d, dev)
+        o = new(Hq * W * d)
     if lse is None and "lse" in want:
-        lse = _f32(Hq * W, dev)
+        lse = new(Hq * W)
     if token_mass is None and "token_mass" in want:
-        token_mass = _f32(kv.n_tokens, dev)
+        token_mass = new(kv.n_tokens)
     pl = pages.view()
     fn = lib().ckv_measure_page_effects_noalloc if noalloc else lib().ckv_measure_page_effects
     ctx.check(fn(ctx.handle, ctypes.byref(kv), ctypes.byref(win), ctypes.byref(pl), _ptr(R),
@@ -447,17 +469,17 @@ def ckv_measure_page_effects_batch(ctx: Context, kvs, wins, pages, *, R=None, wa
     """Problem i: kvs[i], wins[i], pages[i] (Pages).  Returns one dict per
     problem, as ckv_measure_page_effects does."""
     n = len(kvs)
-    dev = torch.device("cuda", ctx.device)
+    new = ctx._outputs()
     outs = []
     for i in range(n):
         Hq, W, d = wins[i].n_q_heads, wins[i].n_rows, kvs[i].head_dim
         np_ = pages[i].n
         outs.append(dict(
-            R=R[i] if R is not None else _f32(max(np_, 1), dev),
-            R_head=_f32(max(np_ * Hq, 1), dev) if "R_head" in want else None,
-            o=_f32(Hq * W * d, dev) if "o" in want else None,
-            lse=_f32(Hq * W, dev) if "lse" in want else None,
-            token_mass=_f32(kvs[i].n_tokens, dev) if "token_mass" in want else None))
+            R=R[i] if R is not None else new(max(np_, 1)),
+            R_head=new(max(np_ * Hq, 1)) if "R_head" in want else None,
+            o=new(Hq * W * d) if "o" in want else None,
+            lse=new(Hq * W) if "lse" in want else None,
+            token_mass=new(kvs[i].n_tokens) if "token_mass" in want else None))
     kv_arr = (KVView * n)(*kvs)
     win_arr = (WindowView * n)(*wins)
     views = [p.view() for p in pages]
@@ -484,16 +506,16 @@ def ckv_measure_recorded(ctx: Context, kv: KVView, win: WindowView, pages: Pages
                          R=None, R_head=None, token_mass=None, want=("R",)):
     """Deletion effect of every page from recorded window outputs o [Hq, W, d]
     and log-sum-exp lse [Hq, W] (float32, device)."""
-    dev = torch.device("cuda", ctx.device)
+    new = ctx._outputs()
     Hq = win.n_q_heads
     if o.dtype != torch.float32 or lse.dtype != torch.float32 or not o.is_contiguous() or not lse.is_contiguous():
         raise ValueError("o and lse must be contiguous float32 tensors")
     if R is None:
-        R = _f32(max(pages.n, 1), dev)
+        R = new(max(pages.n, 1))
     if R_head is None and "R_head" in want:
-        R_head = _f32(max(pages.n * Hq, 1), dev)
+        R_head = new(max(pages.n * Hq, 1))
     if token_mass is None and "token_mass" in want:
-        token_mass = _f32(kv.n_tokens, dev)
+        token_mass = new(kv.n_tokens)
     pl = pages.view()
     ctx.check(lib().ckv_measure_recorded(ctx.handle, ctypes.byref(kv), ctypes.byref(win), ctypes.byref(pl),
                                          _ptr(o), _ptr(lse), _ptr(R), _ptr(R_head), _ptr(token_mass)))
@@ -506,7 +528,7 @@ def ckv_pool_scores(ctx: Context, score, n_tokens, kernel: int = 7, mode: str = 
     if score.dtype != torch.float32 or score.dim() != 2 or score.stride(1) != 1:
         raise ValueError("score must be float32 [n_seq, stride] with a contiguous last axis")
     if out is None:
-        out = torch.zeros_like(score)
+        out = ctx._outputs()(score.shape, make=torch.zeros)
     nt = np.ascontiguousarray(n_tokens, dtype=np.int32)
     ctx.check(lib().ckv_pool_scores(ctx.handle, _ptr(score), _ptr(out), score.shape[0], score.stride(0),
                                     nt.ctypes.data_as(_abi.c_i32p), int(kernel),
@@ -517,15 +539,15 @@ def ckv_pool_scores(ctx: Context, score, n_tokens, kernel: int = 7, mode: str = 
 def ckv_classify_pages(ctx: Context, R_pre, R_post, thresholds: dict | None = None, *,
                        force=None, max_cand: int = 0):
     n = int(R_pre.numel())
-    dev = R_pre.device
+    new = ctx._outputs()
     th = dict(PAPER_THRESHOLDS)
     th.update(thresholds or {})
     t = Thresholds(th["tau_use"], th["tau_dead"], th["rho_use"], th["rho_dead"], th["tau_joint"])
-    lam = torch.empty(max(n, 1), dtype=torch.uint8, device=dev)
-    P_pre = _f32(max(n, 1), dev)
-    P_post = _f32(max(n, 1), dev)
-    cand = torch.empty(max(n, 1), dtype=torch.int32, device=dev)
-    n_cand = torch.empty(1, dtype=torch.int32, device=dev)     # written by the call
+    lam = new(max(n, 1), torch.uint8)
+    P_pre = new(max(n, 1))
+    P_post = new(max(n, 1))
+    cand = new(max(n, 1), torch.int32)
+    n_cand = new(1, torch.int32)     # written by the call
     ctx.check(lib().ckv_classify_pages(ctx.handle, n, _ptr(R_pre), _ptr(R_post), ctypes.byref(t),
                                        _ptr(force), int(max_cand), _ptr(lam), _ptr(P_pre),
                                        _ptr(P_post), _ptr(cand), _ptr(n_cand)))
@@ -534,10 +556,10 @@ def ckv_classify_pages(ctx: Context, R_pre, R_post, thresholds: dict | None = No
 
 def ckv_joint_test(ctx: Context, kv: KVView, win: WindowView, o, lse, pages: Pages, cand, n_cand,
                    max_cand: int, tau_joint: float = 0.01):
-    dev = o.device
-    accepted = torch.empty(max_cand, dtype=torch.uint8, device=dev)
-    union_R = _f32(max_cand, dev)
-    n_acc = torch.empty(1, dtype=torch.int32, device=dev)      # written by the call
+    new = ctx._outputs()
+    accepted = new(max_cand, torch.uint8)
+    union_R = new(max_cand)
+    n_acc = new(1, torch.int32)      # written by the call
     pl = pages.view()
     ctx.check(lib().ckv_joint_test(ctx.handle, ctypes.byref(kv), ctypes.byref(win), _ptr(o),
                                    _ptr(lse), ctypes.byref(pl), _ptr(cand), _ptr(n_cand),
@@ -559,18 +581,18 @@ def ckv_select_and_compact(ctx: Context, k_in, v_in, pos_in, n_tokens, score, re
     compact=False runs the selection only (no output cache; k_in, v_in only
     give the shape)."""
     ns, L, H, cap, d = k_in.shape
-    dev = k_in.device
+    new = ctx._outputs()
     if not compact:
         k_out = v_out = pos_out = None
     elif k_out is None:
-        k_out = torch.empty((ns, L, H, budget, d), dtype=torch.bfloat16, device=dev)
-        v_out = torch.empty_like(k_out)
+        k_out = new((ns, L, H, budget, d), torch.bfloat16)
+        v_out = new((ns, L, H, budget, d), torch.bfloat16)
     if pos_out is None and compact:
-        pos_out = torch.empty((ns, budget), dtype=torch.int32, device=dev)
+        pos_out = new((ns, budget), torch.int32)
     if kept is None:
-        kept = torch.empty((ns, budget), dtype=torch.int32, device=dev)
+        kept = new((ns, budget), torch.int32)
     if n_kept is None:
-        n_kept = torch.empty(ns, dtype=torch.int32, device=dev)   # written by the call
+        n_kept = new(ns, torch.int32)   # written by the call
     cin = cache_view(k_in, v_in, pos_in)
     cout = cache_view(k_out, v_out, pos_out) if compact else None
     acc_arr, keep = None, []
@@ -610,11 +632,11 @@ def _attend_outputs(ctx, views, q, o, lse, want):
     if views[-1].head_dim != q._shape[2]:
         raise ValueError("queries and keys must have the same width")
     if o is None:
-        o = torch.empty(q._shape, dtype=q._torch_dtype, device=q._device)
+        o = ctx._outputs()(q._shape, q._torch_dtype)
     elif o.dtype != q._torch_dtype or o.device != q._device or tuple(o.shape) != q._shape or not o.is_contiguous():
         raise ValueError("o: expected a contiguous tensor of the queries' shape and type")
     if lse is None and "lse" in want:
-        lse = torch.empty(q._shape[:2], dtype=torch.float32, device=q._device)
+        lse = ctx._outputs()(q._shape[:2])
     elif lse is not None and (lse.dtype != torch.float32 or lse.device != q._device or
                               tuple(lse.shape) != q._shape[:2] or not lse.is_contiguous()):
         raise ValueError("lse: expected a contiguous float32 tensor [n_rows, Hq]")
@@ -700,8 +722,10 @@ def ckv_unpack_tokens(ctx: Context, kv: PackedView, *, k=None, v=None, dtype=tor
     if (k is None) != (v is None):
         raise ValueError("k and v are given both or not at all")
     if k is None:
-        shape = (kv.n_seq, kv.n_kv_heads, kv.max_tokens, kv.head_dim)
-        k, v = (torch.zeros(shape, dtype=dtype, device=kv._device) for _ in range(2))
+        if kv._device.index != ctx.device:
+            raise ValueError(f"the caches are on {kv._device}, the context on device {ctx.device}")
+        shape, new = (kv.n_seq, kv.n_kv_heads, kv.max_tokens, kv.head_dim), ctx._outputs()
+        k, v = (new(shape, dtype, torch.zeros) for _ in range(2))
     kind = _check_rows_16(ctx, k, v, 4, kv._device)
     n, hkv, most, d = k.shape
     if n != kv.n_seq or hkv != kv.n_kv_heads or d != kv.head_dim or most < kv.max_tokens:
