@@ -524,12 +524,20 @@ def ckv_measure_recorded(ctx: Context, kv: KVView, win: WindowView, pages: Pages
 
 
 def ckv_pool_scores(ctx: Context, score, n_tokens, kernel: int = 7, mode: str = "max", out=None):
-    """score: float32 [n_seq, stride] (device); n_tokens: ints per sequence."""
+    """score: float32 [n_seq, width] (device); n_tokens: ints per sequence, width at most; out: a tensor of score's shape
+    and strides."""
     if score.dtype != torch.float32 or score.dim() != 2 or score.stride(1) != 1:
         raise ValueError("score must be float32 [n_seq, stride] with a contiguous last axis")
-    if out is None:
-        out = ctx._outputs()(score.shape, make=torch.zeros)
     nt = np.ascontiguousarray(n_tokens, dtype=np.int32)
+    if nt.shape != (score.shape[0],) or (nt.size and nt.max() > score.shape[1]):
+        raise ValueError(f"n_tokens: expected {score.shape[0]} counts of {score.shape[1]} at most")
+    if out is None:
+        # (rows of score and out lie equally far apart)
+        rows = (score.shape[0], score.stride(0)) if score.shape[0] > 1 and score.stride(0) > score.shape[1] else score.shape
+        out = ctx._outputs()(rows, make=torch.zeros)[:, :score.shape[1]]
+    elif out.dtype != torch.float32 or out.device != score.device or out.shape != score.shape or out.stride(1) != 1 or \
+            (len(nt) > 1 and out.stride(0) != score.stride(0)):
+        raise ValueError("out must be like score in type, device, shape and strides")
     ctx.check(lib().ckv_pool_scores(ctx.handle, _ptr(score), _ptr(out), score.shape[0], score.stride(0),
                                     nt.ctypes.data_as(_abi.c_i32p), int(kernel),
                                     {"max": _abi.POOL_MAX, "mean": _abi.POOL_MEAN}[mode]))

@@ -261,6 +261,31 @@ def test_pool_scores(ckv, mode):
         P.ckv_pool_scores(ctx, torch.from_numpy(sc).cuda(), nt, 4, mode)     # even kernel
 
 
+def test_pool_scores_of_part_of_a_tensor(ckv):
+    """Scores inside wider rows: outputs lie in rows as far apart, and what is not like the scores is refused."""
+    P, ctx = ckv
+    rng = np.random.default_rng(10)
+    wide = torch.from_numpy(rng.standard_normal((4, 900)).astype(np.float32)).cuda()
+    score, nt = wide[:, 100:107], [7, 1, 0, 5]
+    given = torch.full((4, 900), 9.0, device="cuda")
+    want = [O.pool_scores(score[s, :n].cpu().numpy(), 3, "max").astype(np.float32) if n else np.zeros(0) for s, n in enumerate(nt)]
+    for out, rest in ((P.ckv_pool_scores(ctx, score, nt, 3), 0), (P.ckv_pool_scores(ctx, score, nt, 3, out=given[:, 100:107]), 9)):
+        ctx.sync()
+        assert out.shape == score.shape
+        for s, n in enumerate(nt):
+            assert np.array_equal(out[s, :n].cpu().numpy(), want[s]) and torch.all(out[s, n:] == rest)
+    assert torch.all(given[:, :100] == 9) and torch.all(given[:, 107:] == 9)
+    one = P.ckv_pool_scores(ctx, score[1:2], [6], 1, out=torch.zeros((1, 7), device="cuda"))
+    ctx.sync()
+    assert torch.equal(one[0, :6], score[1, :6])
+    for bad in (lambda: P.ckv_pool_scores(ctx, score, [7, 1, 0, 8]), lambda: P.ckv_pool_scores(ctx, score, [7, 1, 0]),
+                lambda: P.ckv_pool_scores(ctx, score, nt, out=torch.zeros((4, 7), device="cuda")),
+                lambda: P.ckv_pool_scores(ctx, score, nt, out=given[:3, 100:107]),
+                lambda: P.ckv_pool_scores(ctx, score, nt, out=given.half()[:, 100:107])):
+        with pytest.raises(ValueError):
+            bad()
+
+
 @pytest.mark.parametrize("n_pages,n_cand,max_cand", [(5, 3, 256), (5, 5, 5), (113, 40, 256), (5, 300, 600),
                                                      (300, 290, 400), (1, 0, 7)])
 def test_candidate_counts(ckv, n_pages, n_cand, max_cand):
