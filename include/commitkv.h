@@ -818,8 +818,11 @@ int ckv_unpack_tokens(ckv_ctx* ctx, const ckv_packed_view* kv,
  * values are the fp16 numbers that the codes stand for; which tokens a row sees,
  * outputs, hidden tokens, workspace, capture and errors are as there.
  * Precision: bf16 queries are taken as fp16 times a power of two, one for each
- * row where few rows read a cache, else for up to 32 rows of a sequence: elements
- * below 2^-29 of the largest finite one of these are off by 2^-40 of it at most.
+ * row where few rows read a cache, else one for up to 32 rows of a sequence: an
+ * element is off by 2^-39 of the largest finite one of these at most.  Of rows
+ * whose logits that could tell (where it is more than 2^-25 of a row's own largest)
+ * the 32 are taken again, each with a factor of its own, a token at a time: right,
+ * but some 4 ms for 8192 tokens.
  * Softmax weights are rounded once to fp16 as there (for fp16 outputs of few rows:
  * weight and rest); float32 logits, maxima, sums and accumulation.
  */

@@ -26,7 +26,8 @@ namespace {
 // Output register r of product j is width JW (4q + r) + j.
 //
 // bf16 queries become fp16 times a power of two of their row's own, which its logits
-// are divided by again: their 8 bits fit, and the largest lies below 2^15.
+// are divided by again: the largest lies in [2^14, 2^15), elements keep their 8 bits down
+// to 2^-31 of it, and smaller ones are off by 2^-39 of it at most.
 //
 // Bound: HBM, and latency where there are few tiles a wave.  A tile is 5 KB (16 KB in 16
 // bits) and takes about 270 vector instructions, 1100 of the 2500 cycles or so in which its

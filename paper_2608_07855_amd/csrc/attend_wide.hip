@@ -244,7 +244,7 @@ __device__ __forceinline__ const AttendArgs& fresh_args(const AttendArgs&) {
 }
 
 enum Kept { kS, kRb, kR0, kRows, kX0, kX1 = kX0 + 2, kWork = kX1 + 2, kQmin = kWork + 2, kQmax, kBmin, kBmax, kNextS, kNextRb,
-            kNextX, kLeft = kNextX + 2, kOpening = kLeft + 2, kRecord, kBack = kRecord + 4, kKept };
+            kNextX, kLeft = kNextX + 2, kOpening = kLeft + 2, kRecord, kBack = kRecord + 4, kApart, kKept };
 
 // PRE: the rows of all sequences over the shared tokens, in n_split splits, as
 // partial sums.  Otherwise a share of the blocks (W shares a KV head), in each
@@ -255,7 +255,9 @@ enum Kept { kS, kRb, kR0, kRows, kX0, kX1 = kX0 + 2, kWork = kX1 + 2, kQmin = kW
 // them where a 16-bit tile would have been loaded, for all waves, so that a token is made
 // once for 256 rows.  That goes on between the products with the values (chunks of 8
 // prompts 693 us with a tile made before each step, 658 so).  All products are fp16;
-// bf16 queries become fp16 times a power of two of their wave's 32 rows.
+// bf16 queries become fp16 times a power of two of their wave's 32 rows; where that
+// would lose a row beside one 2^14 as large, the rows are taken again token by token
+// (512 rows on 8192 tokens 0.17 ms, with one such row 4.0).
 template <int D, bool F16, bool TAB, bool PRE, bool PACK>
 __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, SplitSpace sp, int W, int n_split) {
   using L = Wide<D>;
@@ -370,10 +372,14 @@ __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, Sp
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) most = largest_finite(qf[ks], most);
       most = max32(most);
+      const float mine = most;
 #pragma unroll
       for (int off = 16; off; off >>= 1) most = fmaxf(most, __shfl_xor(most, off, 64));
       const PowerOfTwo f = factor_of(most);
       keep(kBack, (int)__float_as_uint(f.back));
+      // fp16 is off by 2^-25 where the wave's largest element is 2^14 or more: by 2^-39 of it.  A row is taken apart where
+      // that is more than 2^-25 of its own largest and (128 keys below 2^16) could move a logit by more than 2^-13.
+      keep(kApart, __ballot(mine > 0.f && mine < most * 0x1p-14f && most * a.sl2 > 8.f) != 0ull);
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) qf[ks] = to_f16(qf[ks], f.mul);
     }
@@ -858,13 +864,28 @@ __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, Sp
     }
     // A token that only some rows of the block see has weight 0 in the others,
     // and 0 times a value that is not finite is NaN: then the share's tokens
-    // are taken again one by one, each by the rows that see it.
+    // are taken again one by one, each by the rows that see it.  So they are where
+    // one factor does not do for the wave's queries, then with a factor for each row.
     bool lost = !__builtin_isfinite(l);
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
       for (int r = 0; r < 16; ++r) lost |= !__builtin_isfinite(o[db][r]);
-    if (hidden && __ballot(lost) != 0ull) {
+    if (__builtin_expect((hidden && __ballot(lost) != 0ull) || (kFactor && get(kApart)), 0)) {
+      float sl2 = b.sl2, mul = 1.f;
+      if constexpr (kFactor) {
+        const int rr = rb2 * kRB + min(wave * 32 + c2, rows2 - 1), p = rr / b.group, h = g * b.group + rr % b.group;
+        const uint16_t* qr = b.q + (int64_t)(r2 + p) * b.q_row_stride + (int64_t)h * b.q_head_stride;
+        float most = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          qf[ks] = ldg_u4(qr + 16 * ks + 8 * hf2);
+          most = largest_finite(qf[ks], most);
+        }
+        const PowerOfTwo f = factor_of(max32(most));
+        mul = f.mul;
+        sl2 *= f.back;
+      }
 #pragma unroll
       for (int db = 0; db < DB; ++db) o[db] = zero16();
       m = -INFINITY;
@@ -884,10 +905,12 @@ __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, Sp
             if constexpr (PACK) kk = row_values<D>(reinterpret_cast<const char*>(kv.k + at), false, 2 * ks + hf2);
             else kk = ldg_u4(kv.k + at + 16 * ks + 8 * hf2);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x = fmaf(elem<C16>(chunk_elem(kk, j)), elem<C16>(chunk_elem(qf[ks], j)), x);
+            for (int j = 0; j < 8; ++j) {
+              float y = elem<F16>(chunk_elem(qf[ks], j));
+              if constexpr (kFactor) y *= mul;
+              x = fmaf(elem<C16>(chunk_elem(kk, j)), y, x);
+            }
           }
-          float sl2 = b.sl2;
-          if constexpr (kFactor) sl2 *= __uint_as_float(get(kBack));
           x = product(sum32(x), sl2);
           if (!(t < pt.row_hi && (t >= pt.row_lo || t < pt.rg.n_first))) continue;
           const float nm = fmaxf(m, x), ref = nm == -INFINITY ? 0.f : nm;
