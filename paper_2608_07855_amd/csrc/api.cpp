@@ -42,9 +42,10 @@ constexpr int kMaxSplitTokens = 8192;
 // itself, and 8 share a launch.
 constexpr size_t kBatchBytes = size_t(384) << 20;
 // Arrival counts of the attention calls, an int an item: only calls of less
-// than 4096 row blocks are split, into 1024 items more and one a KV head.
+// than 4096 row blocks are split, into 1024 items more (caches in 4 bits 1536) and
+// one a KV head.
 constexpr size_t kAttendCounts = size_t(1) << 16;
-// workgroups of up to 512 threads in a launch (a grid has less than 2^32 threads)
+// workgroups of up to 512 threads in a launch (a grid has less than 2^32 threads; the plan that takes 768 bounds itself)
 constexpr int64_t kMostGroups = (int64_t(1) << 23) - 1;
 // the token-mass kernel (126 registers, 40 KB of LDS) keeps two workgroups per
 // compute unit busy: 512 token chunks measured 31.7 us against 35.3 us with 256

@@ -360,7 +360,8 @@ AttendPlan plan_narrow(const AttendArgs& a, int64_t max_tokens, bool room) {
     // Up to a block a compute unit each has a workgroup of 12 waves (32 caches of 4096
     // tokens 36 us, as below 42; 2 row blocks each of 16 caches 46 and 65), unless
     // lengths that may differ by much (32 of up to 32768) would leave most units waiting for a few.
-    p.alone = likely <= 256 && (likely <= 128 || seen <= 8192);
+    // (likely goes by max_rows, an estimate, and a grid, which goes by n_rows, has less than 2^32 threads)
+    p.alone = likely <= 256 && (likely <= 128 || seen <= 8192) && blocks * a.Hkv * 768 < (int64_t(1) << 32);
     p.target = p.alone ? 256 : 1536;
     // Few blocks: splits of 256 tokens for short caches, up to 16 of them (what is joined
     // at once), 768 tokens for long ones (one cache of 8192 tokens 21.7 us, in 32 splits

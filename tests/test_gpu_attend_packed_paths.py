@@ -91,6 +91,24 @@ def test_far_storage(ckv, rows, where):
     check(b, b.run(P, ctx, dict(kv=kv, q=v["q"])), b.want(), where)
 
 
+def test_more_row_blocks_than_large_workgroups_in_a_launch(ckv):
+    """6 million row blocks under an estimate of one row: 2^32 threads are 5.6 million workgroups of 12 waves."""
+    P, ctx = ckv
+    b = PackedBatch(9, [3], [3], 64, 64, 64, qpos=[[0, 1, 2]])
+    v = b.device(P)
+    o3, lse3 = (torch.from_numpy(x).cuda() for x in b.run(P, ctx, v))
+    n = 1500000
+    q = v["q"]._keep[0][:1].expand(n, 64, 64)
+    qpos = (torch.arange(n, device="cuda") % 3).to(torch.int32)
+    view = P.query_view(q, torch.tensor([0, n], dtype=torch.int32, device="cuda"), qpos, max_rows=1)
+    got = P.ckv_attend_packed(ctx, v["kv"], view, want=("o", "lse"))
+    one = P.ckv_attend_packed(ctx, v["kv"], P.query_view(q[:3], torch.tensor([0, 3], dtype=torch.int32, device="cuda"), qpos[:3]), want=("o", "lse"))
+    ctx.sync()
+    assert torch.equal(one["o"][0].double(), o3[0]) and torch.equal(one["lse"][0].double(), lse3[0])
+    for i in range(0, n, 150000):
+        assert torch.all(got["o"][i:i + 150000].view(-1, 3, 64, 64) == one["o"]) and torch.all(got["lse"][i:i + 150000].view(-1, 3, 64) == one["lse"])
+
+
 def test_a_row_beside_larger_ones(ckv):
     """bf16 rows of very different size in one block: each keeps its own logits (to 2^-40 of the largest one's)."""
     for rows in (3, 40):
