@@ -163,6 +163,14 @@ def _ptr(t):
     return ctypes.c_void_p(t.data_ptr()) if t is not None else ctypes.c_void_p(0)
 
 
+def _int32(x, name):
+    """x as an int that the C struct holds (a larger one would lose its upper bits there, without a word)."""
+    x = int(x)
+    if not -2**31 <= x < 2**31:
+        raise ValueError(f"{name} {x} does not fit 32 bits")
+    return x
+
+
 def _check_bf16(t, name, ndim):
     if t.dtype != torch.bfloat16 or not t.is_cuda or t.dim() != ndim or t.stride(-1) != 1:
         raise ValueError(f"{name}: expected a cuda bfloat16 tensor of {ndim} dims with a contiguous last axis")
@@ -188,9 +196,9 @@ def kv_view(k, v, pos, n_tokens: int | None = None, slot=None) -> KVView:
         S = k.shape[1] if n_tokens is None else int(n_tokens)
         if not 1 <= S <= k.shape[1] or pos.numel() < S:
             raise ValueError("n_tokens out of range")
-    view = KVView(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), pos.data_ptr(), S,
-                  k.shape[0], k.shape[2], slot.data_ptr() if slot is not None else None,
-                  k.shape[1] if slot is not None else 0)
+    view = KVView(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), pos.data_ptr(), _int32(S, "n_tokens"),
+                  _int32(k.shape[0], "heads"), k.shape[2], slot.data_ptr() if slot is not None else None,
+                  _int32(k.shape[1], "pool rows") if slot is not None else 0)
     view._keep = (k, v, pos, slot)   # the struct holds raw pointers: keep the tensors alive
     return view
 
@@ -202,8 +210,8 @@ def window_view(q, qpos, scale: float = 0.0) -> WindowView:
         raise ValueError("qpos must be a cuda int32 tensor")
     if qpos.numel() < q.shape[1]:
         raise ValueError("qpos shorter than the window")
-    view = WindowView(q.data_ptr(), q.stride(0), q.stride(1), qpos.data_ptr(), q.shape[0],
-                      q.shape[1], float(scale))
+    view = WindowView(q.data_ptr(), q.stride(0), q.stride(1), qpos.data_ptr(), _int32(q.shape[0], "heads"),
+                      _int32(q.shape[1], "rows"), float(scale))
     view._keep = (q, qpos)
     return view
 
@@ -237,7 +245,7 @@ def cache_view(k, v, pos) -> CacheView:
         raise ValueError("pos must be int32 [n_seq, capacity] with a contiguous last axis")
     s = k.stride()
     view = CacheView(k.data_ptr(), v.data_ptr(), s[0], s[1], s[2], s[3], pos.data_ptr(),
-                     pos.stride(0), k.shape[0], k.shape[1], k.shape[2], k.shape[4], k.shape[3])
+                     pos.stride(0), *(_int32(k.shape[i], "a size of k") for i in (0, 1, 2, 4, 3)))
     view._keep = (k, v, pos)
     return view
 
@@ -258,14 +266,6 @@ def _check_flat(t, name, n, device=None):
     _check_dev(t, name, torch.int32, None, device)
     if not t.is_contiguous() or t.numel() < n:
         raise ValueError(f"{name}: expected a contiguous tensor of {n} entries")
-
-
-def _int32(x, name):
-    """x as an int that the C struct holds (a larger one would lose its upper bits there, without a word)."""
-    x = int(x)
-    if not -2**31 <= x < 2**31:
-        raise ValueError(f"{name} {x} does not fit 32 bits")
-    return x
 
 
 def batch_view(k, v, n_tokens, *, slot=None, pos=None, max_tokens: int | None = None) -> BatchView:
@@ -306,8 +306,9 @@ def batch_view(k, v, n_tokens, *, slot=None, pos=None, max_tokens: int | None = 
     view = BatchView(k.data_ptr(), v.data_ptr(), st[0] if slot is None else 0, st[-3], st[-2],
                      None if slot is None else slot.data_ptr(), 0 if slot is None else slot.stride(0),
                      None if pos is None else pos.data_ptr(), 0 if pos is None else pos.stride(0),
-                     n_tokens.data_ptr(), n, most, 0 if slot is None else k.shape[-2], k.shape[-3], k.shape[-1],
-                     _DTYPES[k.dtype])
+                     n_tokens.data_ptr(), _int32(n, "sequences"), _int32(most, "max_tokens"),
+                     0 if slot is None else _int32(k.shape[-2], "pool rows"), _int32(k.shape[-3], "heads"),
+                     _int32(k.shape[-1], "width"), _DTYPES[k.dtype])
     view._keep = (k, v, n_tokens, slot, pos)   # the struct holds raw pointers: keep the tensors alive
     view._device, view._torch_dtype = k.device, k.dtype
     return view
@@ -355,8 +356,10 @@ def packed_view(pool, n_tokens, *, slot=None, pos=None, max_tokens: int | None =
     st = pool.stride()
     view = PackedView(pool.data_ptr(), st[0] if slot is None else 0, st[-3], st[-2],
                       None if slot is None else slot.data_ptr(), 0 if slot is None else slot.stride(0),
-                      None if pos is None else pos.data_ptr(), 0 if pos is None else pos.stride(0), n_tokens.data_ptr(), n,
-                      most, 0 if slot is None else pool.shape[-2], pool.shape[-3], _PACKED_ROWS[pool.shape[-1]])
+                      None if pos is None else pos.data_ptr(), 0 if pos is None else pos.stride(0), n_tokens.data_ptr(),
+                      _int32(n, "sequences"), _int32(most, "max_tokens"),
+                      0 if slot is None else _int32(pool.shape[-2], "pool rows"), _int32(pool.shape[-3], "heads"),
+                      _PACKED_ROWS[pool.shape[-1]])
     view._keep = (pool, n_tokens, slot, pos)   # the struct holds raw pointers: keep the tensors alive
     view._device = pool.device
     return view
@@ -379,7 +382,8 @@ def query_view(q, cu_rows, qpos=None, *, max_rows: int | None = None, scale: flo
         _check_flat(qpos, "qpos", q.shape[0], q.device)
     most = max(1, -(-q.shape[0] // max(n, 1))) if max_rows is None else _int32(max_rows, "max_rows")
     view = QueryView(q.data_ptr(), q.stride(0), q.stride(1), cu_rows.data_ptr(),
-                     None if qpos is None else qpos.data_ptr(), q.shape[1], q.shape[0], most, float(scale))
+                     None if qpos is None else qpos.data_ptr(), _int32(q.shape[1], "heads"), _int32(q.shape[0], "rows"),
+                     _int32(most, "max_rows"), float(scale))
     view._keep = (q, cu_rows, qpos)
     view._n_seq, view._shape, view._device, view._torch_dtype = n, tuple(q.shape), q.device, q.dtype
     return view
@@ -425,8 +429,8 @@ def slot_step(n_tokens, n_new, free, n_free, slot, *, block_size: int, block_tab
 
     def rows(t):
         return (0, 0) if t is None else (t.stride(0), t.shape[1])
-    step = SlotStep(n, _int32(block_size, "block_size"), free.numel(), max_new, p(n_tokens), p(n_new), p(next_pos), p(n_free),
-                    p(free), p(block_table), *rows(block_table), p(slot), p(pos), *rows(slot), p(n_tokens_out),
+    step = SlotStep(_int32(n, "sequences"), _int32(block_size, "block_size"), _int32(free.numel(), "blocks"), max_new,
+                    p(n_tokens), p(n_new), p(next_pos), p(n_free), p(free), p(block_table), *rows(block_table), p(slot), p(pos), *rows(slot), p(n_tokens_out),
                     p(n_free_out), p(cu_new), p(new_row), p(new_pos), p(status))
     step._keep = (n_tokens, n_new, next_pos, n_free, free, block_table, slot, pos)
     step._device = dev

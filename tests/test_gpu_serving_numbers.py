@@ -41,3 +41,26 @@ def test_the_largest_window(ckv):
     b = Batch(2, [300, 30], [1, 20], 4, 2, 64, gaps=True)
     check(b, b.run(P, ctx, b.device(P), 2**31 - 1, 2**31 - 1), b.want(), "largest")
     check(b, b.run(P, ctx, b.device(P), 2**31 - 1, 0), b.want(), "largest, no first tokens")
+
+
+def test_tables_past_32_bits(ckv):
+    """A table of 2^32 + 8 slots is none of 8; its first ones are there for who asks for them."""
+    P, ctx = ckv
+    far = 2**32 + 8
+    slot = torch.empty((1, far), dtype=torch.int32, device="cuda")
+    slot[0, :20] = torch.arange(20, device="cuda")
+    lens = torch.tensor([20], dtype=torch.int32, device="cuda")
+    pool, k = torch.zeros((2, 20, 80), dtype=torch.uint8, device="cuda"), torch.ones((2, 20, 64), dtype=torch.bfloat16, device="cuda")
+    q, cu = torch.ones((1, 4, 64), dtype=torch.bfloat16, device="cuda"), torch.tensor([0, 1], dtype=torch.int32, device="cuda")
+    for call in (lambda: P.packed_view(pool, lens, slot=slot), lambda: P.packed_view(pool, lens, slot=slot, max_tokens=far),
+                 lambda: P.batch_view(k, k, lens, slot=slot), lambda: P.packed_view(pool[:1].expand(far, 20, 80), lens, slot=slot[:, :20]),
+                 lambda: P.batch_view(k[:1].expand(far, 20, 64), k[:1].expand(far, 20, 64), lens, slot=slot[:, :20]),
+                 lambda: P.query_view(q[:, :1].expand(1, far, 64), cu), lambda: P.query_view(q.expand(far, 4, 64), cu),
+                 lambda: P.kv_view(k, k, slot[0], slot=slot[0])):
+        with pytest.raises(ValueError):
+            call()
+    view = P.query_view(q, cu)
+    o = P.ckv_attend_packed(ctx, P.packed_view(pool, lens, slot=slot, max_tokens=20), view)["o"]
+    p = P.ckv_attend_window(ctx, P.batch_view(k, k, lens, slot=slot, max_tokens=20), view)["o"]
+    ctx.sync()
+    assert not o.any() and torch.all(p == 1)
