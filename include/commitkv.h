@@ -783,15 +783,15 @@ typedef struct ckv_packed_view {
  * ckv_slot_step's new_row).  Tokens from *n_live on (device int32[1], clamped to
  * [0, n_rows]; NULL: n_rows, such as the last entry of cu_new) and tokens whose row lies
  * outside [0, pool_rows) write nothing, so a captured step serves any number of
- * tokens.  Rows of one call must differ; of tokens that share one, its groups
- * hold either's.
+ * tokens.  Rows of one call must differ: one that several tokens name holds a mixture
+ * of them (codes of one under the scale of another) that stands for none.
  *
  * For a group of 32 widths with smallest element m and largest M (elements
  * clamped to [-16384, 16384]), in float32:
  *   s = fp16((M - m) / 15),  b = fp16(m - 16 s) (a zero is +0),  t = x - b,
  *   n = the largest of 1..15 with t >= (15.5 + n) s, or 0,
- * that is the code whose value lies nearest (ties up).  A value differs from its
- * element by s/2 at most, and by what rounding s, b and the value to fp16 adds.
+ * that is the code whose s (16 + n) + b lies nearest (ties up).  A value differs from
+ * its clamped element by s/2 at most, and by what rounding s, b and the value to fp16 adds.
  * A group that holds a NaN or an infinity gets s = 0 and b = NaN: all of it reads
  * back as NaN, and an attention that sees it reports CKV_ERR_NONFINITE.
  * Errors: CKV_ERR_ARG (NULL pointers, alignment, an unknown type, the pool

@@ -709,7 +709,7 @@ def ckv_pack_tokens(ctx: Context, k, v, row, pool, *, n_live=None):
     tokens to 4 bits, token t into row row[t] (int32 [n]) of every head of pool
     (uint8 [Hkv, pool_rows, packed_row_bytes(d)]).  Tokens from n_live[0] on (int32 [1], device;
     None: all live) and tokens whose row lies outside the pool are left out; the rows of
-    the others must differ."""
+    the others must differ (one that several name holds a mixture that stands for none of them)."""
     device = pool.device
     _check_packed(pool, "pool", 3)
     dtype = _check_rows_16(ctx, k, v, 3, device)

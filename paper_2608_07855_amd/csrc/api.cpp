@@ -2028,7 +2028,7 @@ extern "C" int ckv_build_slots(ckv_ctx* c, const ckv_slot_step* st) {
 
 namespace {
 
-// n rows of `st` bytes' distance, as far as they can be told apart; INT64_MAX where they pass it
+// from the first to the last of n rows `st` apart; a quarter of INT64_MAX where that passes it (three of them add up)
 int64_t extent(int64_t n, int64_t st) { return n <= 1 || st == 0 ? 0 : n - 1 > INT64_MAX / 4 / st ? INT64_MAX / 4 : (n - 1) * st; }
 
 int check_packed(ckv_ctx* c, const char* what, const void* data, int64_t seq_stride, int64_t head_stride, int64_t row_stride, int32_t n_kv_heads,

@@ -56,3 +56,24 @@ def test_a_zero_base_has_no_sign(ckv, d):
     v[:, :, ::3] = 0.0                    # both zeros in a group
     got = _packed(ckv, k, v)
     assert np.array_equal(got, O.pack(k.float().numpy(), v.float().numpy())) and not got.any()
+
+
+def test_a_row_named_twice(ckv):
+    """Every 32-bit word of such a row is one of its tokens'; rows named once and rows not named are as ever."""
+    P, ctx = ckv
+    rng = np.random.default_rng(12)
+    n, hkv, d = 3000, 2, 128
+    k, v = (torch.from_numpy(rng.standard_normal((n, hkv, d), dtype=np.float32)).to(torch.bfloat16) for _ in range(2))
+    row = np.arange(n, dtype=np.int32)
+    row[1:1000:2], row[2999] = row[0:999:2], 1500       # neighbours, and tokens of workgroups far apart
+    pool = torch.full((hkv, n, O.row_bytes(d)), 0xA5, dtype=torch.uint8, device="cuda")
+    P.ckv_pack_tokens(ctx, k.cuda(), v.cuda(), torch.from_numpy(row).cuda(), pool)
+    ctx.sync()
+    got = pool.cpu().numpy().transpose(1, 0, 2).copy().view("<u4")
+    each = O.pack(k.float().numpy(), v.float().numpy()).view("<u4")
+    for r in range(n):
+        who = np.flatnonzero(row == r)
+        if len(who) == 0:
+            assert np.all(got[r] == 0xA5A5A5A5)
+        else:
+            assert np.all((got[r][None] == each[who]).any(0)), r
