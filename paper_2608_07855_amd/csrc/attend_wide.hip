@@ -742,21 +742,21 @@ __global__ __launch_bounds__(kNT, 2) void attend_wide_kernel(AttendArgs args, Sp
           if (tile0 + 4 < tile1) load_tables(tile0 + 4);
           if (tile0 + 3 < tile1) load_raw(tile0 + 3);
         } else {
-        find_rows(tile0, rows);
-        load_k(tile0, rows);
-        if (tile0 + 1 < tile1) {
-          find_rows(tile0 + 1, ahead);
-          load_k(tile0 + 1, ahead);
-        }
-        load_v(tile0, rows);
-        if (tile0 + 3 < tile1) load_tables(tile0 + 3);
-        if (tile0 + 1 < tile1) {
-          if (tile0 + 2 < tile1) {
-            find_rows(tile0 + 2, rows);
-            load_k(tile0 + 2, rows);
+          find_rows(tile0, rows);
+          load_k(tile0, rows);
+          if (tile0 + 1 < tile1) {
+            find_rows(tile0 + 1, ahead);
+            load_k(tile0 + 1, ahead);
           }
-          load_v(tile0 + 1, ahead);
-        }
+          load_v(tile0, rows);
+          if (tile0 + 3 < tile1) load_tables(tile0 + 3);
+          if (tile0 + 1 < tile1) {
+            if (tile0 + 2 < tile1) {
+              find_rows(tile0 + 2, rows);
+              load_k(tile0 + 2, rows);
+            }
+            load_v(tile0 + 1, ahead);
+          }
         }
         // What the compiler loaded has to have arrived before the loop, or its own
         // waits inside would drain the tiles under way.

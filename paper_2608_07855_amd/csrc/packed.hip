@@ -50,7 +50,7 @@ __device__ __forceinline__ float as_float(uint32_t bits) {
 // once by its exact remainder.
 //
 // Bound: HBM (4 D bytes in and 1.25 D out a token and head), vector issue close
-// behind (about 12 instructions an element and 40 a thread).  A workgroup takes tokens of
+// behind (75% busy: about 13 instructions an element and 40 a thread).  A workgroup takes tokens of
 // one head, whose rows often follow one another: 65536 tokens of 8 heads of width
 // 128 take 80 us (4.4 TB/s; 8 widths a thread, with 21 instructions an element in all,
 // 94 us; two tokens a thread no less).
