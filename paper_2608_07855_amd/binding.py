@@ -533,6 +533,7 @@ def ckv_pool_scores(ctx: Context, score, n_tokens, kernel: int = 7, mode: str = 
     if score.dtype != torch.float32 or score.dim() != 2 or score.stride(1) != 1:
         raise ValueError("score must be float32 [n_seq, stride] with a contiguous last axis")
     nt = np.ascontiguousarray(n_tokens, dtype=np.int32)
+    nt = nt[:score.shape[0]]
     if nt.shape != (score.shape[0],) or (nt.size and nt.max() > score.shape[1]):
         raise ValueError(f"n_tokens: expected {score.shape[0]} counts of {score.shape[1]} at most")
     if out is None:

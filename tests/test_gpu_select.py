@@ -275,7 +275,7 @@ def test_pool_scores_of_part_of_a_tensor(ckv):
         for s, n in enumerate(nt):
             assert np.array_equal(out[s, :n].cpu().numpy(), want[s]) and torch.all(out[s, n:] == rest)
     assert torch.all(given[:, :100] == 9) and torch.all(given[:, 107:] == 9)
-    one = P.ckv_pool_scores(ctx, score[1:2], [6], 1, out=torch.zeros((1, 7), device="cuda"))
+    one = P.ckv_pool_scores(ctx, score[1:2], [6, 99], 1, out=torch.zeros((1, 7), device="cuda"))
     ctx.sync()
     assert torch.equal(one[0, :6], score[1, :6])
     for bad in (lambda: P.ckv_pool_scores(ctx, score, [7, 1, 0, 8]), lambda: P.ckv_pool_scores(ctx, score, [7, 1, 0]),
